@@ -485,6 +485,118 @@ int vp_unpack_tokens(const int32_t* n_steps_b, const int16_t* lane_dst_b, const 
                      void* out, int32_t* out_map,
                      int32_t* status, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ---- around the AlltoAllv: the operators of a mixture-of-experts layer ------------------------------------------------
+ *
+ * The router in front of it (indices for vp_demand_from_routing and vp_pack, weights for vp_combine), rows in 4 bits on the
+ * way, the experts' products on what vp_unpack writes, and the weighted sum of what vp_unpack_tokens writes.  All of them
+ * enqueue one kernel on cuda_stream of the current device, need no workspace, and wait for nothing; pointers are device
+ * pointers, strides (ld) are in elements, zero tokens or rows are accepted and launch nothing.  Results do not depend on the
+ * launch geometry: sums have a fixed order.
+ */
+
+/* Element types. */
+#define VP_BF16 0
+#define VP_F16  1
+#define VP_F32  2
+
+#define VP_SCORE_SOFTMAX 0
+#define VP_SCORE_SIGMOID 1
+
+typedef struct vp_route_params {
+    int32_t experts;        /* E: all experts, 1 .. 1024                                            */
+    int32_t topk;           /* experts per token, 1 .. 32 and <= topk_group * E / n_group           */
+    int32_t scoring;        /* VP_SCORE_*                                                           */
+    int32_t n_group;        /* groups of E / n_group consecutive experts, 1 .. 32, divides E         */
+    int32_t topk_group;     /* groups a token may use                                               */
+    int32_t group_top;      /* a group is judged by the sum of its best 1 or 2 keys                  */
+    int32_t renormalise;    /* 1: weights are divided by their sum                                  */
+    float   scale;          /* factor of the weights                                                */
+} vp_route_params;
+
+/*
+ * vp_route - experts and weights of T tokens from their router logits.
+ *
+ * Scores are the softmax of a token's logits or 1 / (1 + exp(-logit)); keys are scores + bias (bias: float [E] or NULL; a
+ * balance bias moves the choice and not the weights).  Of the topk_group groups with the largest sums of their best
+ * group_top keys the topk largest keys are chosen, in descending order; the lower index goes first among equal keys, and
+ * among equal groups.  Without a bias keys are the logits.  The choice is the one that keys in 64 bits give.
+ *   logits      [T][ld] of `dtype`, the first E of a row count.  -inf and NaN: the expert cannot be chosen (and has no part in the
+ *               softmax); +inf counts as the largest finite number.  A bias that is -inf or NaN keeps its expert out as well.
+ *   expert_idx  [T][topk] int32; -1 where fewer than topk experts can be chosen (vp_pack drops such copies)
+ *   weights     [T][topk] float; 0 there
+ */
+int vp_route(const vp_route_params* params, const void* logits, int dtype, int64_t ld, int T, const float* bias,
+             int32_t* expert_idx, float* weights, void* cuda_stream);
+
+/*
+ * vp_route_backward - gradient of the weights with respect to the logits, the choice held fixed (the bias has none: it only
+ * moves the choice).  expert_idx [T][topk] as vp_route wrote it (slots that are < 0, >= E or name an expert that cannot be
+ * chosen have no part; one that names an expert a second time adds to it), grad_weights [T][topk] float, grad_logits
+ * [T][grad_ld] of `dtype`: the first E of every row are written.
+ */
+int vp_route_backward(const vp_route_params* params, const void* logits, int dtype, int64_t ld, int T, const int32_t* expert_idx,
+                      const float* grad_weights, void* grad_logits, int64_t grad_ld, void* cuda_stream);
+
+/*
+ * vp_combine - the weighted sum at the end of the layer: out[t] = base[t] + the sum over slots with expert_idx[t][s] >= 0 of
+ * weights[t][s] * rows[t * topk + s], in 32 bits, slots in ascending order, rounded once.
+ *   rows [T * topk][H], base [T][H] or NULL, out [T][H]: of `dtype`, contiguous; out may be base.  Rows of dropped copies
+ *   (expert_idx < 0) are not read.  weights [T][topk] float.
+ */
+int vp_combine(const void* rows, int dtype, const int32_t* expert_idx, const float* weights, int T, int topk, int64_t H,
+               const void* base, void* out, void* cuda_stream);
+
+/*
+ * vp_combine_backward - grad_rows[t * topk + s] = weights[t][s] * grad[t] (0 for dropped copies: what vp_pack sends back) and
+ * grad_weights[t][s] = <grad[t], rows[t * topk + s]> (0 for dropped copies).  Either output may be NULL, rows too when
+ * grad_weights is.  The gradient of base is grad itself.
+ */
+int vp_combine_backward(const void* grad, const void* rows, int dtype, const int32_t* expert_idx, const float* weights, int T,
+                        int topk, int64_t H, void* grad_rows, float* grad_weights, void* cuda_stream);
+
+/*
+ * MXFP4 (OCP Microscaling Formats 1.0): 32 consecutive values of a row share a scale, a power of two held as exponent + 127 in a byte
+ * (255: NaN), and are 4 bits each (+-{0, 0.5, 1, 1.5, 2, 3, 4, 6}), two to a byte, the lower index in the lower half.  A
+ * row of K values is K / 2 bytes of codes and K / 32 of scales.  Kept behind one another in a row of
+ * VP_MXFP4_ROW_BYTES(K) bytes it is what vp_pack and vp_unpack move (4.25 bits a value instead of 16).
+ */
+#define VP_MXFP4_BLOCK 32
+#define VP_MXFP4_ROW_BYTES(K) (((int64_t)(K) / 2 + (int64_t)(K) / 32 + 15) / 16 * 16)
+
+/*
+ * vp_mxfp4_quantize - rows of `dtype` to codes and scales: scale = 2^(floor(log2(largest magnitude of 32)) - 2), at least
+ * 2^-127; code = value / scale to nearest, ties to even, magnitudes above 6 to 6.  A block with an infinity or a NaN gets the
+ * scale 255 and codes 0.
+ *   x       [rows][ld]: cols values per row (a multiple of 32); gated: 2 * cols, and the value quantised is
+ *           silu(x[k]) * x[cols + k] in 32 bits (the activation between an expert's products)
+ *   n_rows  int32[1] or NULL: rows in use (clamped to 0 .. rows); what lies behind them is neither read nor written
+ *   codes   [rows][codes_ld], scales [rows][scales_ld] bytes
+ */
+int vp_mxfp4_quantize(const void* x, int dtype, int64_t ld, int64_t rows, int64_t cols, int gated, const int32_t* n_rows,
+                      uint8_t* codes, int64_t codes_ld, uint8_t* scales, int64_t scales_ld, void* cuda_stream);
+
+/* vp_mxfp4_dequantize - the values that codes and scales stand for, rounded once to `dtype` (exact in bf16 and fp32). */
+int vp_mxfp4_dequantize(const uint8_t* codes, int64_t codes_ld, const uint8_t* scales, int64_t scales_ld, int64_t rows,
+                        int64_t cols, const int32_t* n_rows, void* out, int dtype, int64_t ld, void* cuda_stream);
+
+/*
+ * vp_mxfp4_product - the experts' products: out[r][f] = the sum over k of x[r][k] * w[e][f][k] for the rows expert_off[e] <= r <
+ * expert_off[e + 1] of every expert, products exact, sums in 32 bits, rounded once to `dtype`.
+ *   x_codes    [capacity_rows][x_codes_ld] bytes, x_scales [capacity_rows][x_scales_ld]: expert-major rows (vp_unpack's order) of
+ *              K values; x_codes 16-byte aligned, x_codes_ld a multiple of 16
+ *   w_codes    [E][F][K / 2] (16-byte aligned), w_scales [E][F][K / 32], contiguous: the experts' matrices
+ *   expert_off [E + 1] int32 (vp_unpack's): read on the device.  Rows before the first and behind the last offset are neither
+ *              read nor written.
+ *   out        [capacity_rows][out_ld] of `dtype`; may not overlap the inputs
+ *   status     int32[1], bits are OR-ed in (not cleared): VP_ST_PACK_MISMATCH if an offset falls or lies outside
+ *              0 .. capacity_rows (offsets are then clamped), VP_ST_INTERNAL_TIMEOUT if a bounded wait inside the kernel gave up (out
+ *              is incomplete)
+ * Limits: E <= 1024, K and F <= 2^20, else VP_E_UNSUPPORTED; K a multiple of 32.
+ */
+int vp_mxfp4_product(const uint8_t* x_codes, int64_t x_codes_ld, const uint8_t* x_scales, int64_t x_scales_ld,
+                     int64_t capacity_rows, const uint8_t* w_codes, const uint8_t* w_scales, int E, int64_t F, int64_t K,
+                     const int32_t* expert_off, void* out, int dtype, int64_t out_ld, int32_t* status, void* cuda_stream);
+
 /*
  * How vp_schedule_batch would launch for a batch of B matrices (for benchmarks and tests): out4 (host) receives
  * {kernel, CTAs, threads per CTA, dynamic shared memory bytes}.  kernel 0 = one CTA per matrix; kernel 1 = one

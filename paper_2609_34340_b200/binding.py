@@ -517,6 +517,123 @@ def unpack_tokens(plan: Plan, b: int, rank: int, expert_idx: torch.Tensor, exper
     return status
 
 
+# ---- around the AlltoAllv: router, weighted sum, 4-bit rows, the experts' products ------------------------------------------
+
+@dataclass
+class RouteParams:
+    """Router parameters (``vp_route_params``)."""
+    experts: int
+    topk: int
+    scoring: str = "softmax"
+    n_group: int = 1
+    topk_group: int = 1
+    group_top: int = 1
+    renormalise: bool = True
+    scale: float = 1.0
+
+
+def route(params: RouteParams, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, expert_idx: Optional[torch.Tensor] = None,
+          weights: Optional[torch.Tensor] = None, stream=None):
+    """``vp_route``: the experts and weights of ``[T, experts]`` router logits (bfloat16, float16 or float32).  Returns
+    ``(expert_idx, weights)``, int32 and float32 ``[T, topk]``: what :func:`demand_from_routing`, :func:`pack` and
+    :func:`combine` take.  Not differentiable by itself: see :func:`route_backward`."""
+    if expert_idx is None:
+        expert_idx = torch.empty((logits.shape[0], params.topk), dtype=torch.int32, device=logits.device)
+    if weights is None:
+        weights = torch.empty((logits.shape[0], params.topk), dtype=torch.float32, device=logits.device)
+    rc = (_calls or _load_calls()).route(params, logits, bias, expert_idx, weights, stream)
+    if rc:
+        _check(rc, "vp_route")
+    return expert_idx, weights
+
+
+def route_backward(params: RouteParams, logits: torch.Tensor, expert_idx: torch.Tensor, grad_weights: torch.Tensor,
+                   grad_logits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``vp_route_backward``: gradient of the weights with respect to the logits, for the choice ``expert_idx``."""
+    if grad_logits is None:
+        grad_logits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    rc = (_calls or _load_calls()).route_backward(params, logits, expert_idx, grad_weights, grad_logits, stream)
+    if rc:
+        _check(rc, "vp_route_backward")
+    return grad_logits
+
+
+def combine(rows: torch.Tensor, expert_idx: torch.Tensor, weights: torch.Tensor, base: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``vp_combine``: ``base[t] + sum_s weights[t, s] * rows[t * topk + s]`` over the slots with ``expert_idx >= 0``; ``rows``
+    ``[T * topk, H]`` as :func:`unpack_tokens` writes them."""
+    if out is None:
+        out = torch.empty((expert_idx.shape[0], rows.shape[1]), dtype=rows.dtype, device=rows.device)
+    rc = (_calls or _load_calls()).combine(rows, expert_idx, weights, base, out, stream)
+    if rc:
+        _check(rc, "vp_combine")
+    return out
+
+
+def combine_backward(grad: torch.Tensor, rows: torch.Tensor, expert_idx: torch.Tensor, weights: torch.Tensor,
+                     grad_rows: Optional[torch.Tensor] = None, grad_weights: Optional[torch.Tensor] = None, stream=None):
+    """``vp_combine_backward``: returns ``(grad_rows, grad_weights)`` for the gradient ``[T, H]`` of :func:`combine`'s result."""
+    if grad_rows is None:
+        grad_rows = torch.empty(rows.shape, dtype=rows.dtype, device=rows.device)
+    if grad_weights is None:
+        grad_weights = torch.empty(weights.shape, dtype=torch.float32, device=rows.device)
+    rc = (_calls or _load_calls()).combine_backward(grad, rows, expert_idx, weights, grad_rows, grad_weights, stream)
+    if rc:
+        _check(rc, "vp_combine_backward")
+    return grad_rows, grad_weights
+
+
+def mxfp4_row_bytes(cols: int) -> int:
+    """``VP_MXFP4_ROW_BYTES``: bytes of a row of ``cols`` values with its scales behind its codes, in whole 16 bytes."""
+    return (cols // 2 + cols // 32 + 15) // 16 * 16
+
+
+def mxfp4_rows(rows: torch.Tensor, cols: int):
+    """The two parts ``(codes, scales)`` of a buffer of such rows, uint8 ``[n, mxfp4_row_bytes(cols)]``: what :func:`mxfp4_quantize`
+    writes into rows that :func:`pack` then sends, and what :func:`mxfp4_product` reads of those :func:`unpack` wrote."""
+    return rows[:, :cols // 2], rows[:, cols // 2:cols // 2 + cols // 32]
+
+
+def mxfp4_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, gated: bool = False,
+                   n_rows: Optional[torch.Tensor] = None, stream=None):
+    """``vp_mxfp4_quantize``: rows of ``x`` (``[n, cols]``; ``gated``: ``[n, 2 * cols]``, of which ``silu(first) * second`` is
+    taken) to 4-bit codes ``[n, cols / 2]`` and scales ``[n, cols / 32]``, uint8.  ``n_rows``: int32 on the device, rows in use."""
+    if codes is None or scales is None:
+        cols = x.shape[1] // (2 if gated else 1)
+        assert codes is None and scales is None and cols % 32 == 0, "codes and scales: both or none, for rows of whole blocks of 32 values"
+        codes, scales = mxfp4_rows(torch.empty((x.shape[0], mxfp4_row_bytes(cols)), dtype=torch.uint8, device=x.device), cols)
+    rc = (_calls or _load_calls()).mxfp4_quantize(x, codes, scales, gated, n_rows, stream)
+    if rc:
+        _check(rc, "vp_mxfp4_quantize")
+    return codes, scales
+
+
+def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: Optional[torch.Tensor] = None,
+                     n_rows: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``vp_mxfp4_dequantize``: the values that codes and scales stand for, in ``out``'s type (default bfloat16)."""
+    if out is None:
+        out = torch.empty((codes.shape[0], codes.shape[1] * 2), dtype=torch.bfloat16, device=codes.device)
+    rc = (_calls or _load_calls()).mxfp4_dequantize(codes, scales, out, n_rows, stream)
+    if rc:
+        _check(rc, "vp_mxfp4_dequantize")
+    return out
+
+
+def mxfp4_product(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, expert_off: torch.Tensor,
+                  out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """``vp_mxfp4_product``: expert-major rows times their experts' matrices (codes ``[E, F, K / 2]``, scales ``[E, F, K / 32]``),
+    rows ``expert_off[e] .. expert_off[e + 1]`` with matrix ``e``.  Returns ``(out, status)``: ``[n, F]`` (default bfloat16; rows
+    outside the offsets keep what they hold) and int32[1], into which status bits are OR-ed."""
+    if out is None:
+        out = torch.empty((x_codes.shape[0], w_codes.shape[1]), dtype=torch.bfloat16, device=x_codes.device)
+    if status is None:
+        status = torch.zeros(1, dtype=torch.int32, device=x_codes.device)
+    rc = (_calls or _load_calls()).mxfp4_product(x_codes, x_scales, w_codes, w_scales, expert_off, out, status, stream)
+    if rc:
+        _check(rc, "vp_mxfp4_product")
+    return out, status
+
+
 def prune_paths(topology_blob: bytes) -> bytes:
     """``vp_prune_paths``: the topology blob without its dominated path instances (host code, no GPU)."""
     need, kept = C.c_size_t(0), C.c_int32(0)

@@ -5,6 +5,7 @@
 // time of the call.  Here tensors are unpacked in C++ (about 1 us in all).  Arguments and error codes are those of the C
 // ABI; checks that concern Python arguments raise AssertionError as the Python wrappers do.
 #include <Python.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -47,7 +48,8 @@ struct Ref {                            // an owned reference
 };
 
 #define NAMES(X) X(_h) X(value) X(N) X(lambda_ns) X(granule_bytes) X(k_target) X(n_start) X(i_aa) X(k_max) X(n_steps) X(chan_id) \
-    X(lane_dst) X(lane_inst) X(lane_bytes) X(send_off) X(recv_off) X(tau_ns) X(status) X(cuda_stream)
+    X(lane_dst) X(lane_inst) X(lane_bytes) X(send_off) X(recv_off) X(tau_ns) X(status) X(cuda_stream) \
+    X(experts) X(topk) X(scoring) X(n_group) X(topk_group) X(group_top) X(renormalise) X(scale)
 #define DECLARE(n) PyObject* s_##n;
 NAMES(DECLARE)
 
@@ -249,9 +251,252 @@ PyObject* unpack_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- the operators around the AlltoAllv: tensors on one device, whose current stream is the default ------------------------
+
+struct Device {                         // that device, current for the call
+    c10::Device d;
+    c10::cuda::CUDAGuard guard;
+    explicit Device(const at::Tensor& t) : d(first(t)), guard(d) {}
+    static c10::Device first(const at::Tensor& t) {
+        check(t.is_cuda(), "a device tensor is expected");
+        return t.device();
+    }
+    const at::Tensor& has(const at::Tensor& t) const {
+        check(t.device() == d, "tensors on one device are expected");
+        return t;
+    }
+    void* stream(PyObject* o) const {
+        return o == Py_None ? (void*)c10::cuda::getCurrentCUDAStream(d.index()).stream() : stream_of(o);
+    }
+};
+
+int type_of(const at::Tensor& t) {
+    const auto s = t.scalar_type();
+    check(s == at::kBFloat16 || s == at::kHalf || s == at::kFloat, "bfloat16, float16 or float32 is expected");
+    return s == at::kBFloat16 ? VP_BF16 : (s == at::kHalf ? VP_F16 : VP_F32);
+}
+// Elements from one row to the next of a matrix whose rows are contiguous and do not overlap.
+int64_t row_stride(const at::Tensor& t, const char* text) {
+    check(t.dim() == 2 && (t.size(1) <= 1 || t.stride(1) == 1) && (t.size(0) <= 1 || t.stride(0) >= t.size(1)), text);
+    return t.size(0) <= 1 ? t.size(1) : t.stride(0);
+}
+bool is_matrix(const at::Tensor& t, at::ScalarType s, int64_t rows, int64_t cols) {
+    return t.scalar_type() == s && t.is_contiguous() && t.dim() == 2 && t.size(0) == rows && t.size(1) == cols;
+}
+int int_size(int64_t n) {
+    check(n < ((int64_t)1 << 31), "fewer than 2^31 rows are expected");
+    return (int)n;
+}
+
+vp_route_params route_params_of(PyObject* p) {
+    vp_route_params q;
+    q.experts = (int32_t)attr_int(p, s_experts);
+    q.topk = (int32_t)attr_int(p, s_topk);
+    Ref scoring(PyObject_GetAttr(p, s_scoring));
+    const bool text = PyUnicode_Check(scoring.o);
+    const bool softmax = text && PyUnicode_CompareWithASCIIString(scoring.o, "softmax") == 0;
+    check(softmax || (text && PyUnicode_CompareWithASCIIString(scoring.o, "sigmoid") == 0), "scoring: \"softmax\" or \"sigmoid\"");
+    q.scoring = softmax ? VP_SCORE_SOFTMAX : VP_SCORE_SIGMOID;
+    q.n_group = (int32_t)attr_int(p, s_n_group);
+    q.topk_group = (int32_t)attr_int(p, s_topk_group);
+    q.group_top = (int32_t)attr_int(p, s_group_top);
+    q.renormalise = attr_int(p, s_renormalise) != 0;
+    Ref scale(PyObject_GetAttr(p, s_scale));
+    q.scale = (float)PyFloat_AsDouble(scale.o);
+    if (PyErr_Occurred()) throw Failed{};
+    return q;
+}
+
+// (params, logits, bias, expert_idx, weights, stream)
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 6, [&] {
+        const vp_route_params p = route_params_of(a[0]);
+        const at::Tensor& z = tensor(a[1]);
+        const Device dev(z);
+        const at::Tensor &idx = dev.has(tensor(a[3])), &w = dev.has(tensor(a[4]));
+        const int64_t ld = row_stride(z, "logits: [T, experts], rows contiguous");
+        check(z.size(1) == p.experts, "logits: [T, experts]");
+        check(is_matrix(idx, at::kInt, z.size(0), p.topk) && is_matrix(w, at::kFloat, z.size(0), p.topk),
+              "expert_idx, weights: contiguous int32 and float32 [T, topk]");
+        const void* bias = nullptr;
+        if (a[2] != Py_None) {
+            const at::Tensor& b = dev.has(tensor(a[2]));
+            check(b.scalar_type() == at::kFloat && b.is_contiguous() && b.numel() == p.experts, "bias: contiguous float32 [experts]");
+            bias = b.data_ptr();
+        }
+        const int type = type_of(z), T = int_size(z.size(0));
+        void* stream = dev.stream(a[5]);
+        int rc;
+        WITHOUT_GIL(rc, vp_route(&p, z.data_ptr(), type, ld, T, (const float*)bias, (int32_t*)idx.data_ptr(), (float*)w.data_ptr(), stream))
+        return rc;
+    });
+}
+
+// (params, logits, expert_idx, grad_weights, grad_logits, stream)
+PyObject* route_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 6, [&] {
+        const vp_route_params p = route_params_of(a[0]);
+        const at::Tensor& z = tensor(a[1]);
+        const Device dev(z);
+        const at::Tensor &idx = dev.has(tensor(a[2])), &g = dev.has(tensor(a[3])), &out = dev.has(tensor(a[4]));
+        const int64_t ld = row_stride(z, "logits: [T, experts], rows contiguous"), out_ld = row_stride(out, "grad_logits: [T, experts], rows contiguous");
+        check(z.size(1) == p.experts && out.sizes() == z.sizes() && out.scalar_type() == z.scalar_type(),
+              "logits, grad_logits: [T, experts] of one type");
+        check(is_matrix(idx, at::kInt, z.size(0), p.topk) && is_matrix(g, at::kFloat, z.size(0), p.topk),
+              "expert_idx, grad_weights: contiguous int32 and float32 [T, topk]");
+        const int type = type_of(z), T = int_size(z.size(0));
+        void* stream = dev.stream(a[5]);
+        int rc;
+        WITHOUT_GIL(rc, vp_route_backward(&p, z.data_ptr(), type, ld, T, (const int32_t*)idx.data_ptr(), (const float*)g.data_ptr(),
+                                          out.data_ptr(), out_ld, stream))
+        return rc;
+    });
+}
+
+// (rows, expert_idx, weights, base, out, stream)
+PyObject* combine(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 6, [&] {
+        const at::Tensor& rows = tensor(a[0]);
+        const Device dev(rows);
+        const at::Tensor &idx = dev.has(tensor(a[1])), &w = dev.has(tensor(a[2])), &out = dev.has(tensor(a[4]));
+        check(idx.dim() == 2 && is_matrix(idx, at::kInt, idx.size(0), idx.size(1)) && is_matrix(w, at::kFloat, idx.size(0), idx.size(1)),
+              "expert_idx, weights: contiguous int32 and float32 [T, topk]");
+        const int64_t T = idx.size(0), topk = idx.size(1);
+        check(rows.dim() == 2 && is_matrix(rows, rows.scalar_type(), T * topk, rows.size(1)), "rows: contiguous [T * topk, H]");
+        check(is_matrix(out, rows.scalar_type(), T, rows.size(1)), "out: contiguous [T, H] of the rows' type");
+        const void* base = nullptr;
+        if (a[3] != Py_None) {
+            const at::Tensor& b = dev.has(tensor(a[3]));
+            check(is_matrix(b, rows.scalar_type(), T, rows.size(1)), "base: contiguous [T, H] of the rows' type");
+            base = b.data_ptr();
+        }
+        const int type = type_of(rows), t = int_size(T), k = int_size(topk);
+        void* stream = dev.stream(a[5]);
+        int rc;
+        WITHOUT_GIL(rc, vp_combine(rows.data_ptr(), type, (const int32_t*)idx.data_ptr(), (const float*)w.data_ptr(), t, k, rows.size(1), base,
+                                   out.data_ptr(), stream))
+        return rc;
+    });
+}
+
+// (grad, rows, expert_idx, weights, grad_rows or None, grad_weights or None, stream)
+PyObject* combine_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 7, [&] {
+        const at::Tensor& grad = tensor(a[0]);
+        const Device dev(grad);
+        const at::Tensor &idx = dev.has(tensor(a[2])), &w = dev.has(tensor(a[3]));
+        check(idx.dim() == 2 && is_matrix(idx, at::kInt, idx.size(0), idx.size(1)) && is_matrix(w, at::kFloat, idx.size(0), idx.size(1)),
+              "expert_idx, weights: contiguous int32 and float32 [T, topk]");
+        const int64_t T = idx.size(0), topk = idx.size(1);
+        check(grad.dim() == 2 && is_matrix(grad, grad.scalar_type(), T, grad.size(1)), "grad: contiguous [T, H]");
+        const auto many = [&](PyObject* o, const char* text) -> void* {
+            if (o == Py_None) return nullptr;
+            const at::Tensor& t = dev.has(tensor(o));
+            check(is_matrix(t, grad.scalar_type(), T * topk, grad.size(1)), text);
+            return t.data_ptr();
+        };
+        void *rows = many(a[1], "rows: contiguous [T * topk, H] of the gradient's type"),
+             *grad_rows = many(a[4], "grad_rows: contiguous [T * topk, H] of the gradient's type"), *grad_weights = nullptr;
+        if (a[5] != Py_None) {
+            const at::Tensor& g = dev.has(tensor(a[5]));
+            check(is_matrix(g, at::kFloat, T, topk), "grad_weights: contiguous float32 [T, topk]");
+            grad_weights = g.data_ptr();
+        }
+        const int type = type_of(grad), t = int_size(T), k = int_size(topk);
+        void* stream = dev.stream(a[6]);
+        int rc;
+        WITHOUT_GIL(rc, vp_combine_backward(grad.data_ptr(), rows, type, (const int32_t*)idx.data_ptr(), (const float*)w.data_ptr(), t, k,
+                                            grad.size(1), grad_rows, (float*)grad_weights, stream))
+        return rc;
+    });
+}
+
+const int32_t* count_of(const Device& dev, PyObject* o) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = dev.has(tensor(o));
+    check(t.scalar_type() == at::kInt && t.numel() == 1, "n_rows: one int32 on the device");
+    return (const int32_t*)t.data_ptr();
+}
+// Codes and scales of `rows` rows of `cols` values.
+struct Mx { uint8_t *codes, *scales; int64_t codes_ld, scales_ld; };
+Mx mx_of(const Device& dev, const at::Tensor& c, const at::Tensor& s, int64_t rows, int64_t cols) {
+    dev.has(c);
+    dev.has(s);
+    check(c.scalar_type() == at::kByte && s.scalar_type() == at::kByte, "codes, scales: uint8");
+    const int64_t cl = row_stride(c, "codes: [rows, cols / 2], rows contiguous"), sl = row_stride(s, "scales: [rows, cols / 32], rows contiguous");
+    check(cols % VP_MXFP4_BLOCK == 0, "rows of whole blocks of 32 values are expected");
+    check(c.size(0) == rows && s.size(0) == rows && c.size(1) == cols / 2 && s.size(1) == cols / VP_MXFP4_BLOCK,
+          "codes: [rows, cols / 2], scales: [rows, cols / 32]");
+    return Mx{(uint8_t*)c.data_ptr(), (uint8_t*)s.data_ptr(), cl, sl};
+}
+
+// (x, codes, scales, gated, n_rows, stream)
+PyObject* mxfp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 6, [&] {
+        const at::Tensor& x = tensor(a[0]);
+        const Device dev(x);
+        const int64_t ld = row_stride(x, "x: [rows, cols], rows contiguous");
+        const bool gated = integer(a[3]) != 0;
+        check(!gated || x.size(1) % 2 == 0, "x: [rows, 2 * cols] when gated");
+        const int64_t cols = gated ? x.size(1) / 2 : x.size(1);
+        const Mx m = mx_of(dev, tensor(a[1]), tensor(a[2]), x.size(0), cols);
+        const int32_t* count = count_of(dev, a[4]);
+        const int type = type_of(x);
+        void* stream = dev.stream(a[5]);
+        int rc;
+        WITHOUT_GIL(rc, vp_mxfp4_quantize(x.data_ptr(), type, ld, x.size(0), cols, gated, count, m.codes, m.codes_ld, m.scales, m.scales_ld, stream))
+        return rc;
+    });
+}
+
+// (codes, scales, out, n_rows, stream)
+PyObject* mxfp4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 5, [&] {
+        const at::Tensor& out = tensor(a[2]);
+        const Device dev(out);
+        const int64_t ld = row_stride(out, "out: [rows, cols], rows contiguous");
+        const Mx m = mx_of(dev, tensor(a[0]), tensor(a[1]), out.size(0), out.size(1));
+        const int32_t* count = count_of(dev, a[3]);
+        const int type = type_of(out);
+        void* stream = dev.stream(a[4]);
+        int rc;
+        WITHOUT_GIL(rc, vp_mxfp4_dequantize(m.codes, m.codes_ld, m.scales, m.scales_ld, out.size(0), out.size(1), count, out.data_ptr(), type, ld, stream))
+        return rc;
+    });
+}
+
+// (x_codes, x_scales, w_codes, w_scales, expert_off, out, status, stream)
+PyObject* mxfp4_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 8, [&] {
+        const at::Tensor& wc = tensor(a[2]);
+        const Device dev(wc);
+        const at::Tensor &ws = dev.has(tensor(a[3])), &off = dev.has(tensor(a[4])), &out = dev.has(tensor(a[5])), &st = dev.has(tensor(a[6]));
+        check(wc.scalar_type() == at::kByte && wc.is_contiguous() && wc.dim() == 3, "w_codes: contiguous uint8 [E, F, K / 2]");
+        const int64_t E = wc.size(0), F = wc.size(1), K = wc.size(2) * 2;
+        check(ws.scalar_type() == at::kByte && ws.is_contiguous() && ws.dim() == 3 && ws.size(0) == E && ws.size(1) == F &&
+              ws.size(2) == K / VP_MXFP4_BLOCK, "w_scales: contiguous uint8 [E, F, K / 32]");
+        const int64_t out_ld = row_stride(out, "out: [capacity_rows, F], rows contiguous");
+        check(out.size(1) == F, "out: [capacity_rows, F]");
+        const Mx m = mx_of(dev, tensor(a[0]), tensor(a[1]), out.size(0), K);
+        check(off.scalar_type() == at::kInt && off.is_contiguous() && off.numel() == E + 1, "expert_off: contiguous int32 [E + 1]");
+        check(st.scalar_type() == at::kInt && st.numel() == 1, "status: one int32");
+        const int type = type_of(out), e = int_size(E);
+        // (a single row needs no stride; the kernel's is a multiple of 16)
+        const int64_t codes_ld = out.size(0) <= 1 ? (m.codes_ld + 15) / 16 * 16 : m.codes_ld;
+        void* stream = dev.stream(a[7]);
+        int rc;
+        WITHOUT_GIL(rc, vp_mxfp4_product(m.codes, codes_ld, m.scales, m.scales_ld, out.size(0), (const uint8_t*)wc.data_ptr(),
+                                         (const uint8_t*)ws.data_ptr(), e, F, K, (const int32_t*)off.data_ptr(), out.data_ptr(), type, out_ld,
+                                         (int32_t*)st.data_ptr(), stream))
+        return rc;
+    });
+}
+
 #define METHOD(n) {#n, (PyCFunction)(void*)n, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(schedule_batch), METHOD(schedule_batch_host), METHOD(schedule_batch_host_used), METHOD(demand_from_routing),
-                         METHOD(pack), METHOD(exchange_put), METHOD(unpack), METHOD(unpack_tokens), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(pack), METHOD(exchange_put), METHOD(unpack), METHOD(unpack_tokens),
+                         METHOD(route), METHOD(route_backward), METHOD(combine), METHOD(combine_backward), METHOD(mxfp4_quantize),
+                         METHOD(mxfp4_dequantize), METHOD(mxfp4_product), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,493 @@
+// Routing of tokens to experts (the indices vp_demand_from_routing and vp_pack take, and the weights vp_combine takes) and
+// its gradient.
+//
+// Of the logits z of a token: scores s = softmax(z) or 1 / (1 + exp(-z)), keys = s + bias; with groups, the topk_group groups
+// with the largest sum of their best group_top keys; of what is left the topk largest keys, the lower index among equals.
+// Weights are the scores without the bias, divided by their sum if wanted, times a factor.
+//
+// Which of two experts is chosen hangs on the last bit of a key, so keys in 32 bits, whose error depends on the exponential's
+// code, are not enough to make the choice reproducible.  Without a bias there is nothing to round: scores rise with logits, so
+// logits are compared.  With one, 32-bit keys are computed with a bound on their error; where two keys that matter are nearer
+// than twice that bound and do not come from equal logits and biases, the token is done again in 64 bits.
+#include <cmath>
+#include <type_traits>
+
+#include "elements.cuh"
+
+namespace {
+
+constexpr int kRouteMaxExperts = 1024;
+constexpr int kRouteMaxTop = 32;                  // a lane per chosen expert
+constexpr int kRouteMaxGroups = 32;
+constexpr int kRouteWarps = 4;
+
+struct RouteArgs {
+    const void* logits;
+    long long ld;
+    int T, E, topk;
+    const float* bias;
+    bool sigmoid, renormalise, wide;              // wide: rows can be loaded by vectors
+    int n_group, topk_group, group_top, per;      // per: experts of a group
+    int lanes_per_group;                          // a power of two when groups are whole lanes', else 0
+    float scale;
+    int32_t* idx;
+    float* weights;
+};
+
+// A logit as it counts: -inf for those that cannot be chosen.
+__device__ __forceinline__ float logit_of(float x) { return x > -CUDART_INF_F ? fminf(x, CUDART_MAX_NORMAL_F) : -CUDART_INF_F; }
+
+// Logits of experts lane * VPL .. of one row; -inf for those that cannot be chosen (NaN, -inf, none there).
+template <typename T, int VPL>
+__device__ __forceinline__ void load_logits(const T* row, int E, bool wide, float (&z)[VPL]) {
+    constexpr int most = 16 / (int)sizeof(T);
+    constexpr int V = VPL % 8 == 0 && most >= 8 ? 8 : (VPL % 4 == 0 && most >= 4 ? 4 : (VPL % 2 == 0 ? 2 : 1));
+    const int first = (int)(threadIdx.x & 31) * VPL;
+    T raw[VPL];
+#pragma unroll
+    for (int v = 0; v < VPL; v += V) {
+        if (wide && first + v + V <= E) {
+            const Pack<T, V> p = *(const Pack<T, V>*)(row + first + v);
+#pragma unroll
+            for (int u = 0; u < V; u++) raw[v + u] = p.v[u];
+        } else {
+#pragma unroll
+            for (int u = 0; u < V; u++) raw[v + u] = first + v + u < E ? row[first + v + u] : rounded<T>(-CUDART_INF_F);
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < VPL; v++) z[v] = logit_of(value_of(raw[v]));
+}
+
+// The bias of one expert: one that is not a number above -inf keeps the expert from being chosen.
+__device__ __forceinline__ float bias_of(const float* bias, int e, int E) {
+    const float b = e < E ? bias[e] : 0.f;
+    return b > -CUDART_INF_F ? fminf(b, CUDART_MAX_NORMAL_F) : -CUDART_INF_F;
+}
+
+// Largest and second largest of pairs.
+template <typename K>
+__device__ __forceinline__ void merge_two(K& a, K& b, K c, K d) {
+    const K hi = c > a ? c : a, lo = c > a ? a : c;
+    b = lo > (c > a ? d : b) ? lo : (c > a ? d : b);
+    a = hi;
+}
+template <typename K>
+__device__ __forceinline__ K sum_of_two(K a, K b, int top) {
+    const K none = -(K)CUDART_INF_F;
+    return top > 1 && b > none ? a + b : a;
+}
+
+// The choice for one token in 64 bits, one expert per round; lane r returns the r-th chosen expert or -1.
+template <int VPL>
+__device__ __noinline__ int choose_exactly(const float* zs, const RouteArgs& a) {
+    const int lane = threadIdx.x & 31, first = lane * VPL;
+    const double none = -(double)CUDART_INF_F;
+    double key[VPL], by[VPL];
+    double most = none, total = 0;
+    for (int v = 0; v < VPL; v++) most = fmax(most, (double)zs[v]);
+    for (int o = 16; o; o >>= 1) most = fmax(most, __shfl_xor_sync(kAll, most, o));
+    if (!a.sigmoid) {
+        for (int v = 0; v < VPL; v++) total += zs[v] > -CUDART_INF_F ? exp((double)zs[v] - most) : 0.0;
+        total = warp_sum(total);
+    }
+    for (int v = 0; v < VPL; v++) {
+        const double z = zs[v];
+        const float b = a.bias ? bias_of(a.bias, first + v, a.E) : 0.f;
+        if (!(z > none) || !(b > -CUDART_INF_F)) { key[v] = by[v] = none; continue; }
+        const double s = a.sigmoid ? 1 / (1 + exp(-z)) : exp(z - most) / total;
+        key[v] = a.bias ? s + (double)b : z;
+        by[v] = a.bias || a.group_top > 1 ? s + (double)b : z;
+    }
+    if (a.n_group > 1) {
+        double mine = none;                       // lane g: the score of group g
+        for (int g = 0; g < a.n_group; g++) {
+            double hi = none, lo = none;
+            for (int v = 0; v < VPL; v++) {
+                const int e = first + v;
+                if (e < a.E && e / a.per == g) merge_two(hi, lo, by[v], none);
+            }
+            for (int o = 16; o; o >>= 1) merge_two(hi, lo, __shfl_xor_sync(kAll, hi, o), __shfl_xor_sync(kAll, lo, o));
+            if (lane == g) mine = sum_of_two(hi, lo, a.group_top);
+        }
+        int rank = 0;
+        for (int g = 0; g < a.n_group; g++) {
+            const double other = __shfl_sync(kAll, mine, g);
+            rank += other > mine || (other == mine && g < lane);
+        }
+        const unsigned open = __ballot_sync(kAll, lane < a.n_group && rank < a.topk_group);
+        for (int v = 0; v < VPL; v++)
+            if (first + v < a.E && !(open >> ((first + v) / a.per) & 1)) key[v] = none;
+    }
+    int chosen = -1;
+    for (int r = 0; r < a.topk; r++) {
+        double best = none;
+        int at = kRouteMaxExperts;
+        for (int v = 0; v < VPL; v++)
+            if (key[v] > best) { best = key[v]; at = first + v; }
+        for (int o = 16; o; o >>= 1) {
+            const double other = __shfl_xor_sync(kAll, best, o);
+            const int from = __shfl_xor_sync(kAll, at, o);
+            if (other > best || (other == best && from < at)) { best = other; at = from; }
+        }
+        if (!(best > none)) break;                // (the same in every lane)
+        if (lane == r) chosen = at;
+        for (int v = 0; v < VPL; v++)
+            if (first + v == at) key[v] = none;
+    }
+    return chosen;
+}
+
+// Scores of the chosen (lane r has the r-th, `here` if there is one) up to a factor common to the token, which is 1 unless the
+// weights are divided by their sum: that factor keeps small scores from vanishing in 32 bits.
+__device__ __forceinline__ float chosen_score(bool sigmoid, bool renormalise, bool here, float z, float most, float total) {
+    if (!here) return 0.f;
+    if (!sigmoid) return renormalise ? expf(z - most) : expf(z - most) / total;
+    if (z >= 0) return 1 / (1 + expf(-z));
+    return expf(renormalise ? z - fminf(most, 0.f) : z) / (1 + expf(z));
+}
+
+// A warp per token; lane l holds experts l * VPL .. l * VPL + VPL - 1.  The topk-th largest of the lanes' maxima is a lower bound of
+// the topk-th key, so the few keys above it (about 10 of 256 for the best 8) are put side by side, a lane each, and ranked by counting.
+template <typename T, int VPL>
+__global__ void __launch_bounds__(kRouteWarps * 32)
+route_kernel(const __grid_constant__ RouteArgs a) {
+    extern __shared__ float s_keys[];             // [warps][E], groups that are not whole lanes' only
+    __shared__ float s_key[kRouteWarps][32];
+    __shared__ int s_at[kRouteWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = lane * VPL;
+    grid_wait();
+    const long long t = (long long)blockIdx.x * (blockDim.x >> 5) + warp;
+    if (t >= a.T) return;
+    const T* const row = (const T*)a.logits + t * a.ld;
+    float z[VPL], key[VPL];
+    load_logits<T, VPL>(row, a.E, a.wide, z);
+    float most = -CUDART_INF_F, total = 1;
+    if (!a.sigmoid) {                             // softmax: its largest logit and the sum below it
+#pragma unroll
+        for (int v = 0; v < VPL; v++) most = fmaxf(most, z[v]);
+        most = warp_max(most);
+        const float top = most > -CUDART_INF_F ? most : 0.f;
+        total = 0;
+#pragma unroll
+        for (int v = 0; v < VPL; v++) total += __expf(z[v] - top);
+        total = warp_sum(total);
+    }
+    // keys, and what groups are judged by where that is something else
+    const bool rounded_keys = a.bias != nullptr, rounded_groups = rounded_keys || a.group_top > 1;
+    float tol = 0;
+    float by[VPL];
+#pragma unroll
+    for (int v = 0; v < VPL; v++) key[v] = by[v] = z[v];
+    if (rounded_keys || (a.n_group > 1 && rounded_groups)) {
+        float largest = 0;
+        const float over = __fdividef(1.f, total);
+#pragma unroll
+        for (int v = 0; v < VPL; v++) {
+            const float s = a.sigmoid ? __fdividef(1.f, 1 + __expf(-z[v])) : __expf(z[v] - most) * over;
+            const float b = rounded_keys ? bias_of(a.bias, first + v, a.E) : 0.f;
+            by[v] = z[v] > -CUDART_INF_F && b > -CUDART_INF_F ? s + b : -CUDART_INF_F;
+            if (by[v] > -CUDART_INF_F) largest = fmaxf(largest, fabsf(by[v]));
+            if (rounded_keys) key[v] = by[v];
+        }
+        // Twice a bound of a key's error.  Sigmoid: d s = s (1 - s) d(exp) / exp, with |z| 2^-23 + 2^-21 for the exponential, two units
+        // in the last place for the quotient: below 4e-7.  Softmax: the same for its exponentials (|z - max| s is at most 1/e), 10
+        // additions in a row in the sum: below 1.4e-6 of the largest score.  The sum with the bias: half a unit of the key.
+        tol = 3e-6f * (a.sigmoid ? 1.f : over) + 2.5e-7f * warp_max(largest);
+    }
+    bool unclear = false;
+    if (a.n_group > 1) {
+        float mine = -CUDART_INF_F;
+        unsigned open;
+        const float near = rounded_groups ? 2 * tol : 0.f;
+        if (a.lanes_per_group) {                  // every lane of a group gets its score
+            float hi = -CUDART_INF_F, lo = -CUDART_INF_F;
+#pragma unroll
+            for (int v = 0; v < VPL; v++) merge_two(hi, lo, by[v], -CUDART_INF_F);
+            for (int o = 1; o < a.lanes_per_group; o *= 2) merge_two(hi, lo, __shfl_xor_sync(kAll, hi, o), __shfl_xor_sync(kAll, lo, o));
+            mine = __shfl_sync(kAll, sum_of_two(hi, lo, a.group_top), lane * a.lanes_per_group & 31);
+        } else {
+            float* const k = s_keys + warp * a.E;
+#pragma unroll
+            for (int v = 0; v < VPL; v++)
+                if (first + v < a.E) k[first + v] = by[v];
+            __syncwarp();
+            if (lane < a.n_group) {
+                float hi = -CUDART_INF_F, lo = -CUDART_INF_F;
+                for (int e = lane * a.per; e < (lane + 1) * a.per; e++) merge_two(hi, lo, k[e], -CUDART_INF_F);
+                mine = sum_of_two(hi, lo, a.group_top);
+            }
+        }
+        if (lane >= a.n_group) mine = -CUDART_INF_F;
+        int rank = 0;
+        for (int g = 0; g < a.n_group; g++) {
+            const float other = __shfl_sync(kAll, mine, g);
+            rank += other > mine || (other == mine && g < lane);
+        }
+        const bool in = lane < a.n_group && rank < a.topk_group;
+        open = __ballot_sync(kAll, in);
+        const float worst_in = warp_min(in ? mine : CUDART_INF_F), best_out = warp_max(in ? -CUDART_INF_F : mine);
+        unclear = near > 0 && best_out > -CUDART_INF_F && !(worst_in - best_out > near);
+        if (a.lanes_per_group) {
+            const bool shut = !(open >> (lane / a.lanes_per_group) & 1);
+#pragma unroll
+            for (int v = 0; v < VPL; v++)
+                if (shut) key[v] = -CUDART_INF_F;
+        } else {
+#pragma unroll
+            for (int v = 0; v < VPL; v++)
+                if (first + v < a.E && !(open >> ((first + v) / a.per) & 1)) key[v] = -CUDART_INF_F;
+        }
+    }
+    const float near = rounded_keys ? tol : 0.f;
+    int n = 0;
+    if (!unclear) {
+        float x = -CUDART_INF_F, bound = -CUDART_INF_F;
+#pragma unroll
+        for (int v = 0; v < VPL; v++) x = fmaxf(x, key[v]);
+        for (int r = 0; r < a.topk; r++) {        // (equal maxima leave together: the bound is lower then, and still one)
+            bound = warp_max(x);
+            if (x == bound) x = -CUDART_INF_F;
+        }
+        bound -= near;
+#pragma unroll
+        for (int v = 0; v < VPL; v++) {
+            const bool in = key[v] > -CUDART_INF_F && key[v] >= bound;
+            const unsigned who = __ballot_sync(kAll, in);
+            const int at = n + __popc(who & ((1u << lane) - 1));
+            if (in && at < 32) {
+                s_key[warp][at] = key[v];
+                s_at[warp][at] = first + v;
+            }
+            n += __popc(who);
+        }
+        unclear = n > 32;
+    }
+    __syncwarp();
+    int chosen = -1;
+    if (!unclear) {
+        const float k = lane < n ? s_key[warp][lane] : -CUDART_INF_F;
+        const int at = lane < n ? s_at[warp][lane] : kRouteMaxExperts;
+        int rank = lane < n ? 0 : 32;
+        bool close = false;
+        for (int c = 0; c < n; c++) {
+            const float other = __shfl_sync(kAll, k, c);
+            const int from = __shfl_sync(kAll, at, c);
+            rank += other > k || (other == k && from < at);
+            close |= lane < n && c != lane && fabsf(other - k) <= near;
+        }
+        close = close && near > 0 && rank < a.topk;
+        if (__any_sync(kAll, close)) {            // near: is it the same logit and the same bias?
+            const float my_z = lane < n ? value_of(row[at]) : 0.f, my_b = lane < n ? a.bias[at] : 0.f;
+            bool differ = false;
+            for (int c = 0; c < n; c++) {
+                const float other = __shfl_sync(kAll, k, c), oz = __shfl_sync(kAll, my_z, c), ob = __shfl_sync(kAll, my_b, c);
+                differ |= fabsf(other - k) <= near && (oz != my_z || ob != my_b);
+            }
+            unclear = __any_sync(kAll, close && differ);
+        }
+        __syncwarp();
+        s_at[warp][lane] = -1;
+        __syncwarp();
+        if (rank < a.topk) s_at[warp][rank] = at;
+        __syncwarp();
+        chosen = s_at[warp][lane];
+    }
+    if (unclear) {
+        float copy[VPL];                          // (z itself stays in registers)
+#pragma unroll
+        for (int v = 0; v < VPL; v++) copy[v] = z[v];
+        chosen = choose_exactly<VPL>(copy, a);
+    }
+    const bool here = chosen >= 0;
+    const float zc = here ? logit_of(value_of(row[chosen])) : -CUDART_INF_F;
+    const float top = a.renormalise ? warp_max(zc) : most;
+    float w = chosen_score(a.sigmoid, a.renormalise, here, zc, top, total);
+    if (a.renormalise) {
+        const float sum = warp_sum(w);
+        w = sum > 0 ? w / sum : 0.f;
+    }
+    if (lane < a.topk) {
+        a.idx[t * a.topk + lane] = chosen;
+        a.weights[t * a.topk + lane] = w * a.scale;
+    }
+}
+
+struct RouteGradArgs {
+    const void* logits;
+    long long ld;
+    int T, E, topk;
+    bool sigmoid, renormalise, wide;
+    float scale;
+    const int32_t* idx;
+    const float* grad;
+    void* out;
+    long long out_ld;
+    bool out_wide;
+};
+
+// Gradient of the weights with respect to the logits, the choice held fixed.  With w the weights (scores s, divided by their sum
+// S if they are renormalised) and g the gradient of the weights times the factor:
+//   softmax               dz_i = s_i (g_i - sum_k g_k s_k)            every expert of the row
+//   softmax, renormalised dz_j = w_j (g_j - sum_k g_k w_k)            the chosen, 0 elsewhere
+//   sigmoid               dz_j = g_j s_j (1 - s_j)                    the chosen
+//   sigmoid, renormalised dz_j = w_j (1 - s_j) (g_j - sum_k g_k w_k)  the chosen
+// A warp per token; the row is put together in shared memory and leaves by vectors.
+template <typename T, int VPL>
+__global__ void __launch_bounds__(kRouteWarps * 32)
+route_backward_kernel(const __grid_constant__ RouteGradArgs a) {
+    extern __shared__ float s_rows[];             // [warps][E]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = lane * VPL;
+    grid_wait();
+    const long long t = (long long)blockIdx.x * (blockDim.x >> 5) + warp;
+    if (t >= a.T) return;
+    const T* const row = (const T*)a.logits + t * a.ld;
+    float* const out = s_rows + warp * (32 * VPL);
+    const bool every = !a.sigmoid && !a.renormalise;
+    int at = lane < a.topk ? a.idx[t * a.topk + lane] : -1;
+    float g = lane < a.topk ? a.grad[t * a.topk + lane] * a.scale : 0.f;
+    float z = -CUDART_INF_F;
+    if (at >= 0 && at < a.E) z = logit_of(value_of(row[at]));
+    const bool here = z > -CUDART_INF_F;
+    if (!here) { at = -1; g = 0; }
+    float p[VPL];
+    float most = -CUDART_INF_F, total = 1;
+    if (every) {
+        load_logits<T, VPL>(row, a.E, a.wide, p);
+#pragma unroll
+        for (int v = 0; v < VPL; v++) most = fmaxf(most, p[v]);
+        most = warp_max(most);
+        const float top = most > -CUDART_INF_F ? most : 0.f;
+        total = 0;
+#pragma unroll
+        for (int v = 0; v < VPL; v++) total += p[v] = __expf(p[v] - top);
+        total = warp_sum(total);
+    }
+    const float top = a.renormalise ? warp_max(z) : most;
+    float w = chosen_score(a.sigmoid, a.renormalise, here, z, top, total);
+    if (a.renormalise) {
+        const float sum = warp_sum(w);
+        w = sum > 0 ? w / sum : 0.f;
+    }
+    const bool centred = a.renormalise || !a.sigmoid;
+    const float mean = centred ? warp_sum(g * w) : 0.f;
+    float d = every ? g * w : (a.sigmoid ? w / (1 + expf(z)) * (a.renormalise ? g - mean : g) : w * (g - mean));
+    if (!here) d = 0;
+    const float over = every && total > 0 ? mean / total : 0.f;
+#pragma unroll
+    for (int v = 0; v < VPL; v++) out[first + v] = every ? -p[v] * over : 0.f;
+    __syncwarp();
+    const unsigned same = __match_any_sync(kAll, at);             // an index that stands there twice collects both
+    float sum = 0;
+    if (at >= 0 && __popc(same) > 1) {
+        for (int l = 0; l < 32; l++)
+            if (same >> l & 1) sum += __shfl_sync(same, d, l);
+    } else {
+        sum = d;
+    }
+    if (at >= 0 && (same & ((1u << lane) - 1)) == 0) out[at] += sum;
+    __syncwarp();
+    T* const to = (T*)a.out + t * a.out_ld;
+    constexpr int V = 16 / (int)sizeof(T);
+    if (a.out_wide) {
+        for (int e = lane * V; e < a.E; e += 32 * V) {
+            Pack<T, V> q;
+#pragma unroll
+            for (int u = 0; u < V; u++) q.v[u] = rounded<T>(out[e + u]);
+            *(Pack<T, V>*)(to + e) = q;
+        }
+    } else {
+        for (int e = lane; e < a.E; e += 32) to[e] = rounded<T>(out[e]);
+    }
+}
+
+// Calls fn with the number of experts per lane as a constant.
+template <typename F>
+void with_vpl(int E, F fn) {
+    const int n = (E + 31) / 32;
+#define VPL(k) if (n <= k) return fn(std::integral_constant<int, k>{});
+    VPL(1) VPL(2) VPL(3) VPL(4) VPL(5) VPL(6) VPL(8) VPL(12) VPL(16) VPL(24) VPL(32)
+#undef VPL
+}
+
+int check_route(const vp_route_params* p) {
+    if (!p || p->experts <= 0 || p->topk <= 0 || p->topk > p->experts) return VP_E_BAD_ARG;
+    if (p->scoring != VP_SCORE_SOFTMAX && p->scoring != VP_SCORE_SIGMOID) return VP_E_BAD_ARG;
+    if (p->n_group <= 0 || p->experts % p->n_group || p->topk_group <= 0 || p->topk_group > p->n_group) return VP_E_BAD_ARG;
+    if (p->group_top != 1 && p->group_top != 2) return VP_E_BAD_ARG;
+    if (p->topk > p->topk_group * (p->experts / p->n_group)) return VP_E_BAD_ARG;
+    if (!std::isfinite(p->scale)) return VP_E_BAD_ARG;
+    if (p->experts > kRouteMaxExperts || p->topk > kRouteMaxTop || p->n_group > kRouteMaxGroups) return VP_E_UNSUPPORTED;
+    return VP_OK;
+}
+
+// Whether rows of `ld` elements from `p` on can be moved by vectors of `bytes`.
+bool rows_aligned(const void* p, long long ld, int size, int bytes) {
+    return (uintptr_t)p % bytes == 0 && (unsigned long long)ld * size % bytes == 0;
+}
+
+// A warp per CTA until every SM has work, four beyond: of 128 tokens every one then has an SM nearly to itself.
+int route_warps(int T, int sms) { return T <= 2 * sms ? 1 : kRouteWarps; }
+
+}  // namespace
+
+extern "C" int vp_route(const vp_route_params* p, const void* logits, int dtype, int64_t ld, int T, const float* bias,
+                        int32_t* expert_idx, float* weights, void* cuda_stream) {
+    const int rc = check_route(p);
+    if (rc) return rc;
+    if (!is_type(dtype) || T < 0 || ld < p->experts) return VP_E_BAD_ARG;
+    if ((long long)T * p->topk >= ((long long)1 << 31)) return VP_E_UNSUPPORTED;
+    if (T == 0) return VP_OK;
+    if (!logits || !expert_idx || !weights) return VP_E_BAD_ARG;
+    const int size = size_of_type(dtype);
+    if ((uintptr_t)logits % size) return VP_E_BAD_ARG;
+    const int sms = sm_count_of_device();
+    if (!sms) return VP_E_CUDA;
+    RouteArgs a;
+    a.logits = logits; a.ld = ld; a.T = T; a.E = p->experts; a.topk = p->topk; a.bias = bias;
+    a.sigmoid = p->scoring == VP_SCORE_SIGMOID; a.renormalise = p->renormalise != 0; a.wide = rows_aligned(logits, ld, size, 16);
+    a.n_group = p->n_group; a.topk_group = p->topk_group; a.group_top = p->group_top; a.per = p->experts / p->n_group;
+    a.scale = p->scale; a.idx = expert_idx; a.weights = weights;
+    const int warps = route_warps(T, sms), grid = (T + warps - 1) / warps;
+    cudaError_t e = cudaErrorInvalidValue;
+    with_type(dtype, [&](auto* type) {
+        using X = std::remove_pointer_t<decltype(type)>;
+        with_vpl(a.E, [&](auto vpl) {
+            constexpr int n = decltype(vpl)::value;
+            const int lanes = a.per % n ? 0 : a.per / n;
+            a.lanes_per_group = lanes > 0 && (lanes & (lanes - 1)) == 0 && a.n_group * lanes <= 32 ? lanes : 0;
+            const size_t smem = a.n_group > 1 && !a.lanes_per_group ? (size_t)warps * a.E * 4 : 0;
+            e = launch_after(route_kernel<X, n>, grid, warps * 32, smem, (cudaStream_t)cuda_stream, a);
+        });
+    });
+    return e == cudaSuccess ? VP_OK : VP_E_CUDA;
+}
+
+extern "C" int vp_route_backward(const vp_route_params* p, const void* logits, int dtype, int64_t ld, int T, const int32_t* expert_idx,
+                                 const float* grad_weights, void* grad_logits, int64_t grad_ld, void* cuda_stream) {
+    const int rc = check_route(p);
+    if (rc) return rc;
+    if (!is_type(dtype) || T < 0 || ld < p->experts || grad_ld < p->experts) return VP_E_BAD_ARG;
+    if ((long long)T * p->topk >= ((long long)1 << 31)) return VP_E_UNSUPPORTED;
+    if (T == 0) return VP_OK;
+    if (!logits || !expert_idx || !grad_weights || !grad_logits) return VP_E_BAD_ARG;
+    const int size = size_of_type(dtype);
+    if ((uintptr_t)logits % size || (uintptr_t)grad_logits % size) return VP_E_BAD_ARG;
+    const int sms = sm_count_of_device();
+    if (!sms) return VP_E_CUDA;
+    RouteGradArgs a;
+    a.logits = logits; a.ld = ld; a.T = T; a.E = p->experts; a.topk = p->topk;
+    a.sigmoid = p->scoring == VP_SCORE_SIGMOID; a.renormalise = p->renormalise != 0; a.wide = rows_aligned(logits, ld, size, 16);
+    a.scale = p->scale; a.idx = expert_idx; a.grad = grad_weights; a.out = grad_logits; a.out_ld = grad_ld;
+    a.out_wide = rows_aligned(grad_logits, grad_ld, size, 16) && a.E * size % 16 == 0;
+    const int warps = route_warps(T, sms), grid = (T + warps - 1) / warps;
+    cudaError_t e = cudaErrorInvalidValue;
+    with_type(dtype, [&](auto* type) {
+        using X = std::remove_pointer_t<decltype(type)>;
+        with_vpl(a.E, [&](auto vpl) {
+            constexpr int n = decltype(vpl)::value;
+            e = launch_after(route_backward_kernel<X, n>, grid, warps * 32, (size_t)warps * 32 * n * 4, (cudaStream_t)cuda_stream, a);
+        });
+    });
+    return e == cudaSuccess ? VP_OK : VP_E_CUDA;
+}
