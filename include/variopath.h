@@ -541,7 +541,7 @@ int vp_route_backward(const vp_route_params* params, const void* logits, int dty
  * vp_combine - the weighted sum at the end of the layer: out[t] = base[t] + the sum over slots with expert_idx[t][s] >= 0 of
  * weights[t][s] * rows[t * topk + s], in 32 bits, slots in ascending order, rounded once.
  *   rows [T * topk][H], base [T][H] or NULL, out [T][H]: of `dtype`, contiguous; out may be base.  Rows of dropped copies
- *   (expert_idx < 0) are not read.  weights [T][topk] float.
+ *   (expert_idx < 0) are not read.  weights [T][topk] float.  topk <= 4096, else VP_E_UNSUPPORTED.
  */
 int vp_combine(const void* rows, int dtype, const int32_t* expert_idx, const float* weights, int T, int topk, int64_t H,
                const void* base, void* out, void* cuda_stream);

@@ -26,7 +26,7 @@ struct RouteArgs {
     long long ld;
     int T, E, topk;
     const float* bias;
-    bool sigmoid, renormalise, wide;              // wide: rows can be loaded by vectors
+    bool sigmoid, renormalise, wide, wide_bias;   // wide: rows can be loaded by vectors
     int n_group, topk_group, group_top, per;      // per: experts of a group
     int lanes_per_group;                          // a power of two when groups are whole lanes', else 0
     float scale;
@@ -34,8 +34,8 @@ struct RouteArgs {
     float* weights;
 };
 
-// A logit as it counts: -inf for those that cannot be chosen.
-__device__ __forceinline__ float logit_of(float x) { return x > -CUDART_INF_F ? fminf(x, CUDART_MAX_NORMAL_F) : -CUDART_INF_F; }
+// A logit or a bias as it counts: -inf for NaN (the maximum of a NaN and a number is the number), the largest number for inf.
+__device__ __forceinline__ float logit_of(float x) { return fminf(fmaxf(x, -CUDART_INF_F), CUDART_MAX_NORMAL_F); }
 
 // Logits of experts lane * VPL .. of one row; -inf for those that cannot be chosen (NaN, -inf, none there).
 template <typename T, int VPL>
@@ -59,65 +59,120 @@ __device__ __forceinline__ void load_logits(const T* row, int E, bool wide, floa
     for (int v = 0; v < VPL; v++) z[v] = logit_of(value_of(raw[v]));
 }
 
-// The bias of one expert: one that is not a number above -inf keeps the expert from being chosen.
-__device__ __forceinline__ float bias_of(const float* bias, int e, int E) {
-    const float b = e < E ? bias[e] : 0.f;
-    return b > -CUDART_INF_F ? fminf(b, CUDART_MAX_NORMAL_F) : -CUDART_INF_F;
+// Biases of experts lane * VPL .., 0 without one; -inf keeps an expert from being chosen.
+template <int VPL>
+__device__ __forceinline__ void load_bias(const float* bias, int E, bool wide, float (&b)[VPL]) {
+    constexpr int V = VPL % 4 == 0 ? 4 : (VPL % 2 == 0 ? 2 : 1);
+    const int first = (int)(threadIdx.x & 31) * VPL;
+#pragma unroll
+    for (int v = 0; v < VPL; v += V) {
+        if (wide && first + v + V <= E) {
+            const Pack<float, V> p = *(const Pack<float, V>*)(bias + first + v);
+#pragma unroll
+            for (int u = 0; u < V; u++) b[v + u] = logit_of(p.v[u]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < V; u++) b[v + u] = bias && first + v + u < E ? logit_of(bias[first + v + u]) : 0.f;
+        }
+    }
 }
 
-// Largest and second largest of pairs.
+__device__ __forceinline__ float reciprocal(float x) {           // within a unit in the last place; of infinity 0
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+__device__ __forceinline__ float fast_exp(float x) {             // 2^(x log2 e), the product rounded: |x| 2^-24 + 2^-22, relative
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+    return r;
+}
+
+// Largest and second largest: of a pair and a third value, and of two pairs.
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+__device__ __forceinline__ double smaller(double a, double b) { return fmin(a, b); }
 template <typename K>
-__device__ __forceinline__ void merge_two(K& a, K& b, K c, K d) {
-    const K hi = c > a ? c : a, lo = c > a ? a : c;
-    b = lo > (c > a ? d : b) ? lo : (c > a ? d : b);
-    a = hi;
+__device__ __forceinline__ void insert(K& hi, K& lo, K x) {
+    lo = larger(lo, smaller(hi, x));
+    hi = larger(hi, x);
+}
+template <typename K>
+__device__ __forceinline__ void merge(K& hi, K& lo, K hi2, K lo2) {
+    lo = larger(larger(lo, lo2), smaller(hi, hi2));
+    hi = larger(hi, hi2);
 }
 template <typename K>
 __device__ __forceinline__ K sum_of_two(K a, K b, int top) {
-    const K none = -(K)CUDART_INF_F;
-    return top > 1 && b > none ? a + b : a;
+    return top > 1 && b > -(K)CUDART_INF_F ? a + b : a;
 }
 
-// The choice for one token in 64 bits, one expert per round; lane r returns the r-th chosen expert or -1.
+// What a softmax score in 64 bits is taken from: the largest logit and the sum of the exponentials below it.
+struct Total { double most, sum; };
 template <int VPL>
-__device__ __noinline__ int choose_exactly(const float* zs, const RouteArgs& a) {
-    const int lane = threadIdx.x & 31, first = lane * VPL;
-    const double none = -(double)CUDART_INF_F;
-    double key[VPL], by[VPL];
-    double most = none, total = 0;
+__device__ __forceinline__ Total exact_total(const float* zs, bool sigmoid) {
+    if (sigmoid) return Total{0, 1};
+    double most = -(double)CUDART_INF_F, sum = 0;
     for (int v = 0; v < VPL; v++) most = fmax(most, (double)zs[v]);
     for (int o = 16; o; o >>= 1) most = fmax(most, __shfl_xor_sync(kAll, most, o));
-    if (!a.sigmoid) {
-        for (int v = 0; v < VPL; v++) total += zs[v] > -CUDART_INF_F ? exp((double)zs[v] - most) : 0.0;
-        total = warp_sum(total);
-    }
+    for (int v = 0; v < VPL; v++) sum += zs[v] > -CUDART_INF_F ? exp((double)zs[v] - most) : 0.0;
+    return Total{most, warp_sum(sum)};
+}
+__device__ __forceinline__ double exact_score(float z, bool sigmoid, const Total& t) {
+    return sigmoid ? 1 / (1 + exp(-(double)z)) : exp((double)z - t.most) / t.sum;
+}
+
+// Groups that a token may use, from scores in 64 bits.
+template <int VPL>
+__device__ __noinline__ unsigned open_groups_exactly(const float* zs, const RouteArgs& a) {
+    const int lane = threadIdx.x & 31, first = lane * VPL;
+    const double none = -(double)CUDART_INF_F;
+    const Total total = exact_total<VPL>(zs, a.sigmoid);
+    double by[VPL];
+#pragma unroll
     for (int v = 0; v < VPL; v++) {
-        const double z = zs[v];
-        const float b = a.bias ? bias_of(a.bias, first + v, a.E) : 0.f;
-        if (!(z > none) || !(b > -CUDART_INF_F)) { key[v] = by[v] = none; continue; }
-        const double s = a.sigmoid ? 1 / (1 + exp(-z)) : exp(z - most) / total;
-        key[v] = a.bias ? s + (double)b : z;
-        by[v] = a.bias || a.group_top > 1 ? s + (double)b : z;
+        const float b = a.bias && first + v < a.E ? logit_of(a.bias[first + v]) : 0.f;
+        const bool there = zs[v] > -CUDART_INF_F && b > -CUDART_INF_F;
+        by[v] = there ? exact_score(zs[v], a.sigmoid, total) + (double)b : none;
     }
-    if (a.n_group > 1) {
-        double mine = none;                       // lane g: the score of group g
+    double mine = none;                           // lane g: the score of group g
+    if (a.lanes_per_group) {
+        double hi = none, lo = none;
+#pragma unroll
+        for (int v = 0; v < VPL; v++) insert(hi, lo, by[v]);
+        for (int o = 1; o < a.lanes_per_group; o *= 2) merge(hi, lo, __shfl_xor_sync(kAll, hi, o), __shfl_xor_sync(kAll, lo, o));
+        mine = __shfl_sync(kAll, sum_of_two(hi, lo, a.group_top), lane * a.lanes_per_group & 31);
+    } else {
         for (int g = 0; g < a.n_group; g++) {
             double hi = none, lo = none;
-            for (int v = 0; v < VPL; v++) {
-                const int e = first + v;
-                if (e < a.E && e / a.per == g) merge_two(hi, lo, by[v], none);
-            }
-            for (int o = 16; o; o >>= 1) merge_two(hi, lo, __shfl_xor_sync(kAll, hi, o), __shfl_xor_sync(kAll, lo, o));
+#pragma unroll
+            for (int v = 0; v < VPL; v++)
+                if (first + v < a.E && (first + v) / a.per == g) insert(hi, lo, by[v]);
+            for (int o = 16; o; o >>= 1) merge(hi, lo, __shfl_xor_sync(kAll, hi, o), __shfl_xor_sync(kAll, lo, o));
             if (lane == g) mine = sum_of_two(hi, lo, a.group_top);
         }
-        int rank = 0;
-        for (int g = 0; g < a.n_group; g++) {
-            const double other = __shfl_sync(kAll, mine, g);
-            rank += other > mine || (other == mine && g < lane);
-        }
-        const unsigned open = __ballot_sync(kAll, lane < a.n_group && rank < a.topk_group);
-        for (int v = 0; v < VPL; v++)
-            if (first + v < a.E && !(open >> ((first + v) / a.per) & 1)) key[v] = none;
+    }
+    int rank = 0;
+    for (int g = 0; g < a.n_group; g++) {
+        const double other = __shfl_sync(kAll, mine, g);
+        rank += other > mine || (other == mine && g < lane);
+    }
+    return __ballot_sync(kAll, lane < a.n_group && rank < a.topk_group);
+}
+
+// The choice among the experts `can` marks, one per round, in 64 bits: for tokens with more than 32 candidates (many experts to a
+// lane and most of them shut).  Lane r returns the r-th chosen expert or -1.
+template <int VPL>
+__device__ __noinline__ int choose_by_rounds(const float* zs, unsigned can, const RouteArgs& a) {
+    const int lane = threadIdx.x & 31, first = lane * VPL;
+    const double none = -(double)CUDART_INF_F;
+    const Total total = a.bias ? exact_total<VPL>(zs, a.sigmoid) : Total{0, 1};
+    double key[VPL];
+    for (int v = 0; v < VPL; v++) {
+        const float b = a.bias && first + v < a.E ? a.bias[first + v] : 0.f;
+        key[v] = can >> v & 1 ? (a.bias ? exact_score(zs[v], a.sigmoid, total) + (double)logit_of(b) : (double)zs[v]) : none;
     }
     int chosen = -1;
     for (int r = 0; r < a.topk; r++) {
@@ -138,13 +193,24 @@ __device__ __noinline__ int choose_exactly(const float* zs, const RouteArgs& a) 
     return chosen;
 }
 
+// Rank of the lanes' keys among the first n, the lower index first among equals; 32 from lane n on.
+template <typename K>
+__device__ __forceinline__ int rank_of(K k, int at, int n) {
+    int rank = (int)(threadIdx.x & 31) < n ? 0 : 32;
+    for (int c = 0; c < n; c++) {
+        const K other = __shfl_sync(kAll, k, c);
+        const int from = __shfl_sync(kAll, at, c);
+        rank += other > k || (other == k && from < at);
+    }
+    return rank;
+}
+
 // Scores of the chosen (lane r has the r-th, `here` if there is one) up to a factor common to the token, which is 1 unless the
 // weights are divided by their sum: that factor keeps small scores from vanishing in 32 bits.
-__device__ __forceinline__ float chosen_score(bool sigmoid, bool renormalise, bool here, float z, float most, float total) {
-    if (!here) return 0.f;
-    if (!sigmoid) return renormalise ? expf(z - most) : expf(z - most) / total;
-    if (z >= 0) return 1 / (1 + expf(-z));
-    return expf(renormalise ? z - fminf(most, 0.f) : z) / (1 + expf(z));
+__device__ __forceinline__ float chosen_score(bool sigmoid, bool renormalise, float z, float most, float total) {
+    if (!sigmoid) return renormalise ? fast_exp(z - most) : fast_exp(z - most) * reciprocal(total);
+    const float under = renormalise ? fminf(most, 0.f) : 0.f;          // (a factor of e^-under for every score)
+    return z >= 0 ? reciprocal(1 + fast_exp(-z)) : fast_exp(z - under) * reciprocal(1 + fast_exp(z));
 }
 
 // A warp per token; lane l holds experts l * VPL .. l * VPL + VPL - 1.  The topk-th largest of the lanes' maxima is a lower bound of
@@ -153,7 +219,7 @@ template <typename T, int VPL>
 __global__ void __launch_bounds__(kRouteWarps * 32)
 route_kernel(const __grid_constant__ RouteArgs a) {
     extern __shared__ float s_keys[];             // [warps][E], groups that are not whole lanes' only
-    __shared__ float s_key[kRouteWarps][32];
+    __shared__ alignas(16) float s_key[kRouteWarps][32];
     __shared__ int s_at[kRouteWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = lane * VPL;
     grid_wait();
@@ -170,7 +236,7 @@ route_kernel(const __grid_constant__ RouteArgs a) {
         const float top = most > -CUDART_INF_F ? most : 0.f;
         total = 0;
 #pragma unroll
-        for (int v = 0; v < VPL; v++) total += __expf(z[v] - top);
+        for (int v = 0; v < VPL; v++) total += fast_exp(z[v] - top);
         total = warp_sum(total);
     }
     // keys, and what groups are judged by where that is something else
@@ -181,30 +247,36 @@ route_kernel(const __grid_constant__ RouteArgs a) {
     for (int v = 0; v < VPL; v++) key[v] = by[v] = z[v];
     if (rounded_keys || (a.n_group > 1 && rounded_groups)) {
         float largest = 0;
-        const float over = __fdividef(1.f, total);
+        const float over = a.sigmoid ? 1.f : reciprocal(total);
+        float b[VPL];
+        load_bias<VPL>(a.bias, a.E, a.wide_bias, b);
 #pragma unroll
         for (int v = 0; v < VPL; v++) {
-            const float s = a.sigmoid ? __fdividef(1.f, 1 + __expf(-z[v])) : __expf(z[v] - most) * over;
-            const float b = rounded_keys ? bias_of(a.bias, first + v, a.E) : 0.f;
-            by[v] = z[v] > -CUDART_INF_F && b > -CUDART_INF_F ? s + b : -CUDART_INF_F;
-            if (by[v] > -CUDART_INF_F) largest = fmaxf(largest, fabsf(by[v]));
+            const float k = (a.sigmoid ? reciprocal(1 + fast_exp(-z[v])) : fast_exp(z[v] - most) * over) + b[v];
+            largest = fmaxf(largest, fabsf(k));
+            by[v] = z[v] > -CUDART_INF_F ? k : -CUDART_INF_F;
             if (rounded_keys) key[v] = by[v];
+        }
+        largest = warp_max(largest);
+        if (!(largest < CUDART_INF_F)) {          // a bias of -inf, or no logit
+            largest = 0;
+#pragma unroll
+            for (int v = 0; v < VPL; v++)
+                if (by[v] > -CUDART_INF_F) largest = fmaxf(largest, fabsf(by[v]));
+            largest = warp_max(largest);
         }
         // Twice a bound of a key's error.  Sigmoid: d s = s (1 - s) d(exp) / exp, with |z| 2^-23 + 2^-21 for the exponential, two units
         // in the last place for the quotient: below 4e-7.  Softmax: the same for its exponentials (|z - max| s is at most 1/e), 10
         // additions in a row in the sum: below 1.4e-6 of the largest score.  The sum with the bias: half a unit of the key.
-        tol = 3e-6f * (a.sigmoid ? 1.f : over) + 2.5e-7f * warp_max(largest);
+        tol = 3e-6f * over + 2.5e-7f * largest;
     }
-    bool unclear = false;
     if (a.n_group > 1) {
         float mine = -CUDART_INF_F;
-        unsigned open;
-        const float near = rounded_groups ? 2 * tol : 0.f;
         if (a.lanes_per_group) {                  // every lane of a group gets its score
             float hi = -CUDART_INF_F, lo = -CUDART_INF_F;
 #pragma unroll
-            for (int v = 0; v < VPL; v++) merge_two(hi, lo, by[v], -CUDART_INF_F);
-            for (int o = 1; o < a.lanes_per_group; o *= 2) merge_two(hi, lo, __shfl_xor_sync(kAll, hi, o), __shfl_xor_sync(kAll, lo, o));
+            for (int v = 0; v < VPL; v++) insert(hi, lo, by[v]);
+            for (int o = 1; o < a.lanes_per_group; o *= 2) merge(hi, lo, __shfl_xor_sync(kAll, hi, o), __shfl_xor_sync(kAll, lo, o));
             mine = __shfl_sync(kAll, sum_of_two(hi, lo, a.group_top), lane * a.lanes_per_group & 31);
         } else {
             float* const k = s_keys + warp * a.E;
@@ -214,7 +286,7 @@ route_kernel(const __grid_constant__ RouteArgs a) {
             __syncwarp();
             if (lane < a.n_group) {
                 float hi = -CUDART_INF_F, lo = -CUDART_INF_F;
-                for (int e = lane * a.per; e < (lane + 1) * a.per; e++) merge_two(hi, lo, k[e], -CUDART_INF_F);
+                for (int e = lane * a.per; e < (lane + 1) * a.per; e++) insert(hi, lo, k[e]);
                 mine = sum_of_two(hi, lo, a.group_top);
             }
         }
@@ -225,9 +297,16 @@ route_kernel(const __grid_constant__ RouteArgs a) {
             rank += other > mine || (other == mine && g < lane);
         }
         const bool in = lane < a.n_group && rank < a.topk_group;
-        open = __ballot_sync(kAll, in);
-        const float worst_in = warp_min(in ? mine : CUDART_INF_F), best_out = warp_max(in ? -CUDART_INF_F : mine);
-        unclear = near > 0 && best_out > -CUDART_INF_F && !(worst_in - best_out > near);
+        unsigned open = __ballot_sync(kAll, in);
+        if (rounded_groups) {                     // is the last group in clear of the first one out?
+            const float worst_in = warp_min(in ? mine : CUDART_INF_F), best_out = warp_max(in ? -CUDART_INF_F : mine);
+            if (best_out > -CUDART_INF_F && !(worst_in - best_out > 2 * tol)) {
+                float copy[VPL];                  // (z itself stays in registers)
+#pragma unroll
+                for (int v = 0; v < VPL; v++) copy[v] = z[v];
+                open = open_groups_exactly<VPL>(copy, a);
+            }
+        }
         if (a.lanes_per_group) {
             const bool shut = !(open >> (lane / a.lanes_per_group) & 1);
 #pragma unroll
@@ -240,72 +319,100 @@ route_kernel(const __grid_constant__ RouteArgs a) {
         }
     }
     const float near = rounded_keys ? tol : 0.f;
-    int n = 0;
-    if (!unclear) {
-        float x = -CUDART_INF_F, bound = -CUDART_INF_F;
+    float x = -CUDART_INF_F, bound = -CUDART_INF_F;
 #pragma unroll
-        for (int v = 0; v < VPL; v++) x = fmaxf(x, key[v]);
-        for (int r = 0; r < a.topk; r++) {        // (equal maxima leave together: the bound is lower then, and still one)
-            bound = warp_max(x);
-            if (x == bound) x = -CUDART_INF_F;
-        }
-        bound -= near;
-#pragma unroll
-        for (int v = 0; v < VPL; v++) {
-            const bool in = key[v] > -CUDART_INF_F && key[v] >= bound;
-            const unsigned who = __ballot_sync(kAll, in);
-            const int at = n + __popc(who & ((1u << lane) - 1));
-            if (in && at < 32) {
-                s_key[warp][at] = key[v];
-                s_at[warp][at] = first + v;
-            }
-            n += __popc(who);
-        }
-        unclear = n > 32;
+    for (int v = 0; v < VPL; v++) x = fmaxf(x, key[v]);
+    for (int r = 0; r < a.topk; r++) {            // (equal maxima leave together: the bound is lower then, and still one)
+        bound = warp_max(x);
+        if (x == bound) x = -CUDART_INF_F;
     }
-    __syncwarp();
-    int chosen = -1;
-    if (!unclear) {
-        const float k = lane < n ? s_key[warp][lane] : -CUDART_INF_F;
-        const int at = lane < n ? s_at[warp][lane] : kRouteMaxExperts;
-        int rank = lane < n ? 0 : 32;
-        bool close = false;
-        for (int c = 0; c < n; c++) {
-            const float other = __shfl_sync(kAll, k, c);
-            const int from = __shfl_sync(kAll, at, c);
-            rank += other > k || (other == k && from < at);
-            close |= lane < n && c != lane && fabsf(other - k) <= near;
-        }
-        close = close && near > 0 && rank < a.topk;
-        if (__any_sync(kAll, close)) {            // near: is it the same logit and the same bias?
-            const float my_z = lane < n ? value_of(row[at]) : 0.f, my_b = lane < n ? a.bias[at] : 0.f;
-            bool differ = false;
-            for (int c = 0; c < n; c++) {
-                const float other = __shfl_sync(kAll, k, c), oz = __shfl_sync(kAll, my_z, c), ob = __shfl_sync(kAll, my_b, c);
-                differ |= fabsf(other - k) <= near && (oz != my_z || ob != my_b);
+    bound = fmaxf(bound - near, -CUDART_MAX_NORMAL_F);
+    // Candidates side by side, in the order of their indices: places by a scan over the lanes' counts.
+    unsigned mine = 0;
+#pragma unroll
+    for (int v = 0; v < VPL; v++) mine |= (unsigned)(key[v] >= bound) << v;
+    int n = __popc(mine);
+    const int own = n;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int other = __shfl_up_sync(kAll, n, o);
+        if (lane >= o) n += other;
+    }
+    int place = n - own;
+    n = __shfl_sync(kAll, n, 31);
+    int chosen;
+    if (n <= 32) {
+        s_key[warp][lane] = -CUDART_INF_F;
+        __syncwarp();
+#pragma unroll
+        for (int v = 0; v < VPL; v++)
+            if (mine >> v & 1) {
+                s_key[warp][place] = key[v];
+                s_at[warp][place] = first + v;
+                place++;
             }
-            unclear = __any_sync(kAll, close && differ);
+        __syncwarp();
+        const float k = s_key[warp][lane];
+        const int at = lane < n ? s_at[warp][lane] : kRouteMaxExperts;
+        int rank = 0;
+#pragma unroll 1
+        for (int c = 0; c < n; c += 4) {          // (places behind the n-th hold -inf)
+            const float4 q = *(const float4*)&s_key[warp][c];
+            rank += (q.x > k || (q.x == k && c < lane)) + (q.y > k || (q.y == k && c + 1 < lane)) +
+                    (q.z > k || (q.z == k && c + 2 < lane)) + (q.w > k || (q.w == k && c + 3 < lane));
+        }
+        if (lane >= n) rank = lane;
+        if (near > 0) {
+            // Keys in descending order: is one that is not clearly below the topk-th near the one behind it, and not from the same
+            // logit and bias?  (Of equal ones the lower index goes first, which is right.)
+            __syncwarp();
+            s_key[warp][rank] = k;
+            __syncwarp();
+            const float here = s_key[warp][lane], last = s_key[warp][min(a.topk, n) - 1 & 31];
+            const float behind = lane < 31 ? s_key[warp][lane + 1] : -CUDART_INF_F;
+            const bool close = lane + 1 < n && here - behind <= near && here >= last - near;
+            if (__any_sync(kAll, close)) {
+                const float my_z = lane < n ? logit_of(value_of(row[at])) : 0.f, my_b = lane < n ? logit_of(a.bias[at]) : 0.f;
+                const unsigned where = __ballot_sync(kAll, close);
+                bool differ = false;
+                for (int r = 0; r < 31; r++)
+                    if (where >> r & 1) {         // (the same in every lane)
+                        const int up = __ffs(__ballot_sync(kAll, rank == r)) - 1, down = __ffs(__ballot_sync(kAll, rank == r + 1)) - 1;
+                        differ |= __shfl_sync(kAll, my_z, up) != __shfl_sync(kAll, my_z, down) ||
+                                  __shfl_sync(kAll, my_b, up) != __shfl_sync(kAll, my_b, down);
+                    }
+                if (differ) {
+                    float copy[VPL];
+#pragma unroll
+                    for (int v = 0; v < VPL; v++) copy[v] = z[v];
+                    const Total all = exact_total<VPL>(copy, a.sigmoid);
+                    rank = rank_of(lane < n ? exact_score(my_z, a.sigmoid, all) + (double)my_b : -(double)CUDART_INF_F, at, n);
+                }
+            }
         }
         __syncwarp();
         s_at[warp][lane] = -1;
         __syncwarp();
-        if (rank < a.topk) s_at[warp][rank] = at;
+        if (lane < n && rank < a.topk) s_at[warp][rank] = at;
         __syncwarp();
         chosen = s_at[warp][lane];
-    }
-    if (unclear) {
-        float copy[VPL];                          // (z itself stays in registers)
+    } else {
+        float copy[VPL];
+        unsigned can = 0;                         // bit v: expert first + v can be chosen
 #pragma unroll
-        for (int v = 0; v < VPL; v++) copy[v] = z[v];
-        chosen = choose_exactly<VPL>(copy, a);
+        for (int v = 0; v < VPL; v++) {
+            copy[v] = z[v];
+            can |= (unsigned)(key[v] > -CUDART_INF_F) << v;
+        }
+        chosen = choose_by_rounds<VPL>(copy, can, a);
     }
     const bool here = chosen >= 0;
     const float zc = here ? logit_of(value_of(row[chosen])) : -CUDART_INF_F;
     const float top = a.renormalise ? warp_max(zc) : most;
-    float w = chosen_score(a.sigmoid, a.renormalise, here, zc, top, total);
+    float w = here ? chosen_score(a.sigmoid, a.renormalise, zc, top, total) : 0.f;
     if (a.renormalise) {
         const float sum = warp_sum(w);
-        w = sum > 0 ? w / sum : 0.f;
+        w = sum > 0 ? w * reciprocal(sum) : 0.f;
     }
     if (lane < a.topk) {
         a.idx[t * a.topk + lane] = chosen;
@@ -360,14 +467,14 @@ route_backward_kernel(const __grid_constant__ RouteGradArgs a) {
         const float top = most > -CUDART_INF_F ? most : 0.f;
         total = 0;
 #pragma unroll
-        for (int v = 0; v < VPL; v++) total += p[v] = __expf(p[v] - top);
+        for (int v = 0; v < VPL; v++) total += p[v] = fast_exp(p[v] - top);
         total = warp_sum(total);
     }
     const float top = a.renormalise ? warp_max(z) : most;
-    float w = chosen_score(a.sigmoid, a.renormalise, here, z, top, total);
+    float w = here ? chosen_score(a.sigmoid, a.renormalise, z, top, total) : 0.f;
     if (a.renormalise) {
         const float sum = warp_sum(w);
-        w = sum > 0 ? w / sum : 0.f;
+        w = sum > 0 ? w * reciprocal(sum) : 0.f;
     }
     const bool centred = a.renormalise || !a.sigmoid;
     const float mean = centred ? warp_sum(g * w) : 0.f;
@@ -446,6 +553,7 @@ extern "C" int vp_route(const vp_route_params* p, const void* logits, int dtype,
     RouteArgs a;
     a.logits = logits; a.ld = ld; a.T = T; a.E = p->experts; a.topk = p->topk; a.bias = bias;
     a.sigmoid = p->scoring == VP_SCORE_SIGMOID; a.renormalise = p->renormalise != 0; a.wide = rows_aligned(logits, ld, size, 16);
+    a.wide_bias = bias && (uintptr_t)bias % 16 == 0;
     a.n_group = p->n_group; a.topk_group = p->topk_group; a.group_top = p->group_top; a.per = p->experts / p->n_group;
     a.scale = p->scale; a.idx = expert_idx; a.weights = weights;
     const int warps = route_warps(T, sms), grid = (T + warps - 1) / warps;
