@@ -6,6 +6,7 @@
 //
 // Both are bound by HBM: every row is read once (and its gradient written once), in 16-byte vectors, all slots of a vector in
 // flight at once.  Sums are in 32 bits, slots in ascending order; a dropped copy's row is not read (its memory may hold anything).
+// The sum of 16,384 tokens x 8 rows of 7,168 bf16: 324 us, 6.5 TB/s.
 #include <type_traits>
 
 #include "elements.cuh"
@@ -13,7 +14,8 @@
 namespace {
 
 constexpr int kCombineThreads = 256;
-constexpr int kSlots = 8;                         // slots whose rows are in flight together
+constexpr int kSlots = 8;                         // slots whose rows are in flight together, at most
+constexpr int kGradThreads = 64, kGradStages = 5;  // (three to six stages, two or four warps: within 3 %)
 constexpr int kCombineMaxTop = 4096;              // (8 bytes of shared memory per slot)
 
 // A vector of a row that is there, zeros for one that is not (its memory may hold anything): loads under a predicate, no branch
@@ -45,7 +47,7 @@ struct CombineArgs {
 
 // A CTA takes a piece of `tokens` tokens side by side: their indices and weights are fetched once, which otherwise stands in front of
 // every load of a row.  16,384 tokens x 8 of 7,168 bf16: one token per CTA 417 us.
-template <typename T, int V>
+template <typename T, int V, int S>
 __global__ void __launch_bounds__(kCombineThreads, 4)
 combine_kernel(const __grid_constant__ CombineArgs a) {
     extern __shared__ int2 s_slot[];              // per slot: whether it counts, its weight
@@ -70,11 +72,11 @@ combine_kernel(const __grid_constant__ CombineArgs a) {
 #pragma unroll
             for (int u = 0; u < V; u++) sum[u] = value_of(x.v[u]);
         }
-        for (int s0 = 0; s0 < a.topk; s0 += kSlots) {
-            Pack<T, V> x[kSlots];
-            float w[kSlots];
+        for (int s0 = 0; s0 < a.topk; s0 += S) {
+            Pack<T, V> x[S];
+            float w[S];
 #pragma unroll
-            for (int s = 0; s < kSlots; s++) {
+            for (int s = 0; s < S; s++) {
                 const int slot = min(s0 + s, a.topk - 1);
                 const int2 q = s_slot[(int)k * a.topk + slot];
                 const bool here = q.x && s0 + s < a.topk;
@@ -82,7 +84,7 @@ combine_kernel(const __grid_constant__ CombineArgs a) {
                 x[s] = load_if<T, V>(rows + slot * a.H, here);
             }
 #pragma unroll
-            for (int s = 0; s < kSlots; s++)
+            for (int s = 0; s < S; s++)
 #pragma unroll
                 for (int u = 0; u < V; u++) sum[u] = fmaf(w[s], value_of(x[s].v[u]), sum[u]);
         }
@@ -100,68 +102,118 @@ struct CombineGradArgs {
     void* grad_rows;
     float* grad_weights;
     long long T, H;
-    int topk, warps;                              // warps that share a token (a power of two)
+    int topk;
 };
 
-// `warps` warps per token and kSlots slots, so that a thread has a few vectors; every thread keeps its part of the slots' inner products,
-// which meet in a fixed order.
-template <typename T, int V>
-__global__ void __launch_bounds__(kCombineThreads)
+// 16 bytes to shared memory while the thread goes on; zeros where there is nothing to copy (nothing is read then).
+__device__ __forceinline__ void copy_16(unsigned to, const void* from, bool here) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(here ? 16 : 0) : "memory");
+}
+
+// A warp per token and S slots.  Every lane copies the vectors that it will work on itself, kGradStages - 1 steps of 32 vectors ahead, so
+// that nothing waits for another thread and the loads in flight cost no registers: with loads into registers, one step at a time or two,
+// reads and writes together reached 4.9 to 6.1 TB/s (8,192 tokens x 8 of 4,096 bf16 186 to 235 us, 1,531 x 6 of 2,048 18 to 22); so 6.3 TB/s, 181 and
+// 17.4 us.
+template <typename T, int S>
+__global__ void __launch_bounds__(kGradThreads)
 combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
-    __shared__ float s_part[kCombineThreads / 32][kSlots];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per_cta = kCombineThreads / 32 / a.warps;
+    constexpr int V = 16 / (int)sizeof(T);
+    extern __shared__ uint4 s_stage[];            // [warps][stages][S + 1][32]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_wait();
-    const int batches = (a.topk + kSlots - 1) / kSlots;
-    const long long item = (long long)blockIdx.x * per_cta + warp / a.warps, t = item / batches;
-    const bool in = t < a.T;
-    const int s0 = (int)(item % batches) * kSlots, slots = in ? min(kSlots, a.topk - s0) : 0;
-    const long long first = t * a.topk + s0, n = in ? a.H / V : 0;
-    const T *const grad = (const T*)a.grad + t * a.H, *const rows = (const T*)a.rows + first * a.H;
-    T* const grad_rows = (T*)a.grad_rows + first * a.H;
-    bool here[kSlots];
-    float w[kSlots], dot[kSlots];
+    const int batches = (a.topk + S - 1) / S;
+    const long long item = (long long)blockIdx.x * (kGradThreads / 32) + warp, t = item / batches;
+    if (t >= a.T) return;
+    const int s0 = (int)(item % batches) * S, slots = min(S, a.topk - s0);
+    const long long first = t * a.topk + s0, n = a.H / V;
+    const int at = lane < slots ? a.idx[first + lane] : -1;
+    const float own = at >= 0 ? a.weights[first + lane] : 0.f;
+    const unsigned here = __ballot_sync(kAll, at >= 0), read = a.grad_weights ? here : 0;
+    const uint4 *const grad = (const uint4*)a.grad + t * n, *const rows = (const uint4*)a.rows + first * n;
+    uint4* const grad_rows = (uint4*)a.grad_rows + first * n;
+    uint4* const stage = s_stage + warp * kGradStages * (S + 1) * 32 + lane;
+    const unsigned stage_at = (unsigned)__cvta_generic_to_shared(stage);
+    const auto issue = [&](long long i, int k) {
+        const unsigned to = stage_at + k * (S + 1) * 512;
+        copy_16(to, grad + i, i < n);
 #pragma unroll
-    for (int s = 0; s < kSlots; s++) {
-        here[s] = s < slots && a.idx[first + s] >= 0;
-        w[s] = here[s] ? a.weights[first + s] : 0.f;
+        for (int s = 0; s < S; s++) copy_16(to + (s + 1) * 512, rows + s * n + i, i < n && (read >> s & 1));
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    float w[S], dot[S];
+#pragma unroll
+    for (int s = 0; s < S; s++) {
+        w[s] = __shfl_sync(kAll, own, s);
         dot[s] = 0;
     }
-    for (long long i = (warp % a.warps) * 32 + lane; i < n; i += a.warps * 32) {
-        const Pack<T, V> g = *(const Pack<T, V>*)(grad + i * V);
-        Pack<T, V> x[kSlots];
-        if (a.grad_weights)
 #pragma unroll
-            for (int s = 0; s < kSlots; s++) x[s] = load_if<T, V>(rows + (here[s] ? s : 0) * a.H + i * V, here[s]);
-        if (a.grad_rows)
+    for (int k = 0; k < kGradStages - 1; k++) issue(lane + 32 * k, k);
+    int k = 0;
+    for (long long i = lane; __any_sync(kAll, i < n); i += 32) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kGradStages - 2) : "memory");
+        const uint4* const from = stage + k * (S + 1) * 32;
+        const Pack<T, V> g = *(const Pack<T, V>*)from;
+        float f[V];
 #pragma unroll
-            for (int s = 0; s < kSlots; s++)
-                if (s < slots) {
-                    Pack<T, V> y;
+        for (int u = 0; u < V; u++) f[u] = value_of(g.v[u]);
 #pragma unroll
-                    for (int u = 0; u < V; u++) y.v[u] = rounded<T>(here[s] ? w[s] * value_of(g.v[u]) : 0.f);
-                    *(Pack<T, V>*)(grad_rows + s * a.H + i * V) = y;
-                }
-        if (a.grad_weights)
+        for (int s = 0; s < S; s++) {
+            const Pack<T, V> x = *(const Pack<T, V>*)(from + (s + 1) * 32);
 #pragma unroll
-            for (int s = 0; s < kSlots; s++)
+            for (int u = 0; u < V; u++) dot[s] = fmaf(f[u], value_of(x.v[u]), dot[s]);
+        }
+        const int last = k == 0 ? kGradStages - 1 : k - 1;
+        issue(i + 32 * (kGradStages - 1), last);
+        if (a.grad_rows && i < n)
 #pragma unroll
-                for (int u = 0; u < V; u++) dot[s] = fmaf(value_of(g.v[u]), value_of(x[s].v[u]), dot[s]);
+            for (int s = 0; s < S; s++) {
+                const bool is = here >> s & 1;    // (0 times an infinity is not 0)
+                Pack<T, V> y;
+#pragma unroll
+                for (int u = 0; u < V; u++) y.v[u] = rounded<T>(is ? w[s] * f[u] : 0.f);
+                if (s < slots) *(Pack<T, V>*)(grad_rows + s * n + i) = y;
+            }
+        if (++k == kGradStages) k = 0;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (!a.grad_weights) return;
     float mine = 0;
 #pragma unroll
-    for (int s = 0; s < kSlots; s++) {
+    for (int s = 0; s < S; s++) {
         const float d = warp_sum(dot[s]);
         if (lane == s) mine = d;
     }
-    if (a.warps > 1) {
-        if (lane < kSlots) s_part[warp][lane] = mine;
-        __syncthreads();
-        mine = 0;
-        if (warp % a.warps == 0 && lane < kSlots)
-            for (int k = 0; k < a.warps; k++) mine += s_part[warp + k][lane];
+    if (lane < slots) a.grad_weights[first + lane] = mine;
+}
+
+// The same value by value, for rows that do not begin on 16-byte borders.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads)
+combine_backward_plain_kernel(const __grid_constant__ CombineGradArgs a) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    grid_wait();
+    const long long item = (long long)blockIdx.x * (kGradThreads / 32) + warp, t = item / a.topk;
+    if (t >= a.T) return;
+    const bool here = a.idx[item] >= 0;
+    const float w = here ? a.weights[item] : 0.f;
+    const T *const grad = (const T*)a.grad + t * a.H, *const row = (const T*)a.rows + item * a.H;
+    float dot = 0;
+    for (long long i = lane; i < a.H; i += 32) {
+        const float f = value_of(grad[i]);
+        if (here && a.grad_weights) dot = fmaf(f, value_of(row[i]), dot);
+        if (a.grad_rows) ((T*)a.grad_rows)[item * a.H + i] = rounded<T>(here ? w * f : 0.f);
     }
-    if (warp % a.warps == 0 && lane < slots) a.grad_weights[first + lane] = mine;
+    dot = warp_sum(dot);
+    if (lane == 0 && a.grad_weights) a.grad_weights[item] = dot;
+}
+
+// Calls fn with the slots that are in flight together as a constant.
+template <typename F>
+void with_slots(int topk, F fn) {
+    if (topk > 6) return fn(std::integral_constant<int, kSlots>{});
+    if (topk > 4) return fn(std::integral_constant<int, 6>{});
+    if (topk > 2) return fn(std::integral_constant<int, 4>{});
+    return topk > 1 ? fn(std::integral_constant<int, 2>{}) : fn(std::integral_constant<int, 1>{});
 }
 
 // Vectors of 16 bytes where rows begin on such borders, single values elsewhere.
@@ -199,8 +251,11 @@ extern "C" int vp_combine(const void* rows, int dtype, const int32_t* expert_idx
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        e = launch_after(wide ? combine_kernel<X, 16 / (int)sizeof(X)> : combine_kernel<X, 1>, (int)(groups * pieces), threads, (size_t)a.tokens * topk * 8,
-                         (cudaStream_t)cuda_stream, a);
+        with_slots(wide ? topk : kSlots, [&](auto slots) {
+            constexpr int s = decltype(slots)::value;
+            e = launch_after(wide ? combine_kernel<X, 16 / (int)sizeof(X), s> : combine_kernel<X, 1, kSlots>, (int)(groups * pieces), threads,
+                             (size_t)a.tokens * topk * 8, (cudaStream_t)cuda_stream, a);
+        });
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
 }
@@ -213,17 +268,23 @@ extern "C" int vp_combine_backward(const void* grad, const void* rows, int dtype
     if (!grad || !expert_idx || !weights || (!grad_rows && !grad_weights) || (grad_weights && !rows)) return VP_E_BAD_ARG;
     const int size = size_of_type(dtype);
     if ((uintptr_t)grad % size || (uintptr_t)rows % size || (uintptr_t)grad_rows % size) return VP_E_BAD_ARG;
-    CombineGradArgs a{grad, rows, expert_idx, weights, grad_rows, grad_weights, T, H, topk, 1};
+    const CombineGradArgs a{grad, rows, expert_idx, weights, grad_rows, grad_weights, T, H, topk};
     const bool wide = vectors(size, H, {grad, rows, grad_rows});
-    const long long n = wide ? H * size / 16 : H;
-    while (a.warps < kCombineThreads / 32 && n > 4 * 32 * a.warps) a.warps *= 2;        // about four vectors a thread
-    const int per_cta = kCombineThreads / 32 / a.warps;
-    const long long items = (long long)T * ((topk + kSlots - 1) / kSlots), grid = (items + per_cta - 1) / per_cta;
+    const auto ctas = [&](long long items) { return (int)((items + kGradThreads / 32 - 1) / (kGradThreads / 32)); };
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        e = launch_after(wide ? combine_backward_kernel<X, 16 / (int)sizeof(X)> : combine_backward_kernel<X, 1>, (int)grid, kCombineThreads, 0,
-                         (cudaStream_t)cuda_stream, a);
+        if (!wide) {
+            e = launch_after(combine_backward_plain_kernel<X>, ctas((long long)T * topk), kGradThreads, 0, (cudaStream_t)cuda_stream, a);
+            return;
+        }
+        with_slots(topk, [&](auto slots) {
+            constexpr int s = decltype(slots)::value;
+            constexpr size_t smem = (size_t)(kGradThreads / 32) * kGradStages * (s + 1) * 512;
+            const auto fn = combine_backward_kernel<X, s>;
+            e = smem > 48 * 1024 ? cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+            if (e == cudaSuccess) e = launch_after(fn, ctas((long long)T * ((topk + s - 1) / s)), kGradThreads, smem, (cudaStream_t)cuda_stream, a);
+        });
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
 }

@@ -14,7 +14,8 @@
 namespace {
 
 constexpr int kMxThreads = 256;
-constexpr int kMxPer = 8;                         // values per thread: four threads share a scale
+constexpr int kMxPer = 8;                         // values of a thread's piece: four threads share a scale
+constexpr int kMxPieces = 4;                      // pieces of a thread, all loaded before the first is worked on
 
 struct MxArgs {
     const void* x;
@@ -22,7 +23,9 @@ struct MxArgs {
     uint8_t *codes, *scales;
     long long codes_ld, scales_ld;
     const int32_t* n_rows;                        // rows in use, on the device; null: all
-    long long R, K, groups;                       // groups of kMxPer values per row
+    long long R, K;
+    int groups;                                   // of kMxPer values per row
+    SmallDiv by_groups;
     bool wide, wide_codes;
 };
 
@@ -58,79 +61,95 @@ __device__ __forceinline__ unsigned codes_of(float lo, float hi) {
 // 2^e, -127 <= e <= 127.
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float(e > -127 ? (e + 127) << 23 : 1 << 22); }
 
-// A thread per eight values.  GATED: rows are 2 K wide, the value is silu(x[k]) * x[K + k], in 32 bits.
+// Row and piece of a row of the CTA's u-th piece of this thread; false behind the last row in use.  A CTA's pieces are consecutive.
+struct Piece { long long r; int c; };
+__device__ __forceinline__ bool piece_of(const MxArgs& a, long long r0, int c0, long long rows, int u, Piece& p) {
+    const int i = c0 + u * kMxThreads + (int)threadIdx.x, down = a.by_groups.div(i);
+    p.r = r0 + down;
+    p.c = i - down * a.groups;
+    return p.r < rows;
+}
+
+// GATED: rows are 2 K wide, the value is silu(x[k]) * x[K + k], in 32 bits.
 template <typename T, bool GATED>
 __global__ void __launch_bounds__(kMxThreads)
 mxfp4_quantize_kernel(const __grid_constant__ MxArgs a) {
     grid_wait();
-    const long long n = rows_in_use(a.n_rows, a.R) * a.groups, step = (long long)gridDim.x * kMxThreads;
-    // four threads of a block of 32 values are neighbours and groups is a multiple of four, so they stay in the loop together;
-    // a warp's last lanes may leave it, hence the ballot
-    for (long long i = (long long)blockIdx.x * kMxThreads + threadIdx.x; __any_sync(kAll, i < n); i += step) {
-        const bool in = i < n;
-        const long long r = in ? i / a.groups : 0, c = in ? i % a.groups : 0;
-        float x[kMxPer];
-        if (in) {
-            const T* const at = (const T*)a.x + r * a.ld + c * kMxPer;
-            load_eight<T>(at, a.wide, x);
-            if (GATED) {
-                float u[kMxPer];
-                load_eight<T>(at + a.K, a.wide, u);
+    const long long rows = rows_in_use(a.n_rows, a.R), i0 = (long long)blockIdx.x * (kMxThreads * kMxPieces), r0 = i0 / a.groups;
+    if (r0 >= rows) return;
+    const int c0 = (int)(i0 - r0 * a.groups);
+    Piece p[kMxPieces];
+    bool in[kMxPieces];
+    float x[kMxPieces][kMxPer], up[GATED ? kMxPieces : 1][kMxPer];
 #pragma unroll
-                for (int v = 0; v < kMxPer; v++) x[v] = x[v] / (1 + expf(-x[v])) * u[v];
-            }
-        } else {
+    for (int u = 0; u < kMxPieces; u++) {
+        in[u] = piece_of(a, r0, c0, rows, u, p[u]);
+        const T* const at = (const T*)a.x + (in[u] ? p[u].r * a.ld + p[u].c * kMxPer : 0);      // (the first is in use)
+        load_eight<T>(at, a.wide, x[u]);
+        if (GATED) load_eight<T>(at + a.K, a.wide, up[u]);
+    }
 #pragma unroll
-            for (int v = 0; v < kMxPer; v++) x[v] = 0;
-        }
+    for (int u = 0; u < kMxPieces; u++) {
+        if (GATED)
+#pragma unroll
+            for (int v = 0; v < kMxPer; v++) x[u][v] = x[u][v] / (1 + expf(-x[u][v])) * up[u][v];
         unsigned most = 0;                        // of magnitudes as bits: their order is that of the values, NaN above all
 #pragma unroll
-        for (int v = 0; v < kMxPer; v++) most = max(most, __float_as_uint(x[v]) & 0x7fffffffu);
-        most = max(most, __shfl_xor_sync(kAll, most, 1));
+        for (int v = 0; v < kMxPer; v++) most = max(most, __float_as_uint(x[u][v]) & 0x7fffffffu);
+        most = max(most, __shfl_xor_sync(kAll, most, 1));        // (groups is a multiple of four: a block's threads are neighbours)
         most = max(most, __shfl_xor_sync(kAll, most, 2));
         const bool finite = most < 0x7f800000u;
         const int e = max((int)(most >> 23) - 129, -127);        // (magnitudes below 2^-125, zero among them: 2^-127)
         const float inverse = power_of_two(-e);
         unsigned word = 0;
-        if (finite)
 #pragma unroll
-            for (int v = 0; v < kMxPer; v += 2) word |= codes_of(x[v] * inverse, x[v + 1] * inverse) << (4 * v);
-        if (in) {
-            uint8_t* const to = a.codes + r * a.codes_ld + c * (kMxPer / 2);
+        for (int v = 0; v < kMxPer; v += 2) word |= codes_of(x[u][v] * inverse, x[u][v + 1] * inverse) << (4 * v);
+        if (!finite) word = 0;
+        if (in[u]) {
+            uint8_t* const to = a.codes + p[u].r * a.codes_ld + p[u].c * (kMxPer / 2);
             if (a.wide_codes) *(unsigned*)to = word;
             else
 #pragma unroll
                 for (int b = 0; b < 4; b++) to[b] = (uint8_t)(word >> (8 * b));
-            if ((c & 3) == 0) a.scales[r * a.scales_ld + c / 4] = finite ? (uint8_t)(e + 127) : 255;
+            if ((p[u].c & 3) == 0) a.scales[p[u].r * a.scales_ld + p[u].c / 4] = finite ? (uint8_t)(e + 127) : 255;
         }
     }
 }
 
-// A thread per eight values, to the values they stand for, rounded once to T (exact in bf16 and fp32).
+// To the values that codes and scales stand for, rounded once to T (exact in bf16 and fp32).
 template <typename T>
 __global__ void __launch_bounds__(kMxThreads)
 mxfp4_dequantize_kernel(const __grid_constant__ MxArgs a) {
     grid_wait();
-    const long long n = rows_in_use(a.n_rows, a.R) * a.groups, step = (long long)gridDim.x * kMxThreads;
-    for (long long i = (long long)blockIdx.x * kMxThreads + threadIdx.x; i < n; i += step) {
-        const long long r = i / a.groups, c = i % a.groups;
-        const uint8_t* const from = a.codes + r * a.codes_ld + c * (kMxPer / 2);
-        unsigned word = 0;
-        if (a.wide_codes) word = *(const unsigned*)from;
-        else
+    const long long rows = rows_in_use(a.n_rows, a.R), i0 = (long long)blockIdx.x * (kMxThreads * kMxPieces), r0 = i0 / a.groups;
+    if (r0 >= rows) return;
+    const int c0 = (int)(i0 - r0 * a.groups);
+    Piece p[kMxPieces];
+    bool in[kMxPieces];
+    unsigned word[kMxPieces];
+    int s[kMxPieces];
 #pragma unroll
-            for (int b = 0; b < 4; b++) word |= (unsigned)from[b] << (8 * b);
-        const int s = a.scales[r * a.scales_ld + c / 4];
-        const float scale = s == 255 ? CUDART_NAN_F : power_of_two(s - 127);
+    for (int u = 0; u < kMxPieces; u++) {
+        in[u] = piece_of(a, r0, c0, rows, u, p[u]);
+        if (!in[u]) p[u] = Piece{r0, 0};
+        const uint8_t* const from = a.codes + p[u].r * a.codes_ld + p[u].c * (kMxPer / 2);
+        if (a.wide_codes) word[u] = *(const unsigned*)from;
+        else word[u] = (unsigned)from[0] | (unsigned)from[1] << 8 | (unsigned)from[2] << 16 | (unsigned)from[3] << 24;
+        s[u] = a.scales[p[u].r * a.scales_ld + p[u].c / 4];
+    }
+#pragma unroll
+    for (int u = 0; u < kMxPieces; u++) {
+        const float scale = s[u] == 255 ? CUDART_NAN_F : power_of_two(s[u] - 127);
         alignas(16) T y[kMxPer];
 #pragma unroll
         for (int v = 0; v < kMxPer; v += 2) {
-            const __half2 h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(word >> (4 * v)), __NV_E2M1);
+            const __half2 h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(word[u] >> (4 * v)), __NV_E2M1);
             y[v] = rounded<T>(__low2float(h) * scale);
             y[v + 1] = rounded<T>(__high2float(h) * scale);
         }
-        T* const to = (T*)a.x + r * a.ld + c * kMxPer;
+        T* const to = (T*)a.x + p[u].r * a.ld + p[u].c * kMxPer;
         constexpr int V = 16 / (int)sizeof(T);
+        if (!in[u]) continue;
         if (a.wide) {
 #pragma unroll
             for (int v = 0; v < kMxPer; v += V) *(Pack<T, V>*)(to + v) = *(const Pack<T, V>*)(y + v);
@@ -150,15 +169,12 @@ int fill(MxArgs& a, const void* x, int dtype, int64_t ld, int64_t width, int64_t
     if (!x || !codes || !scales) return VP_E_BAD_ARG;
     const int size = size_of_type(dtype);
     if ((uintptr_t)x % size) return VP_E_BAD_ARG;
-    a = MxArgs{x, ld, (uint8_t*)codes, (uint8_t*)scales, codes_ld, scales_ld, n_rows, R, K, K / kMxPer,
+    a = MxArgs{x, ld, (uint8_t*)codes, (uint8_t*)scales, codes_ld, scales_ld, n_rows, R, K, (int)(K / kMxPer), small_div((int)(K / kMxPer)),
                (uintptr_t)x % 16 == 0 && ld * size % 16 == 0, (uintptr_t)codes % 4 == 0 && codes_ld % 4 == 0};
     return VP_OK;
 }
 
-int mx_grid(const MxArgs& a, int sms) {
-    const long long want = (a.R * a.groups + kMxThreads - 1) / kMxThreads, most = (long long)sms * 64;
-    return (int)(want < most ? want : most);
-}
+long long mx_grid(const MxArgs& a) { return (a.R * a.groups + kMxThreads * kMxPieces - 1) / (kMxThreads * kMxPieces); }
 
 }  // namespace
 
@@ -167,12 +183,12 @@ extern "C" int vp_mxfp4_quantize(const void* x, int dtype, int64_t ld, int64_t r
     MxArgs a;
     const int rc = fill(a, x, dtype, ld, gated ? 2 * cols : cols, rows, cols, codes, codes_ld, scales, scales_ld, n_rows);
     if (rc || rows == 0) return rc;
-    const int sms = sm_count_of_device();
-    if (!sms) return VP_E_CUDA;
+    const long long grid = mx_grid(a);
+    if (grid >= ((long long)1 << 31)) return VP_E_UNSUPPORTED;
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        e = launch_after(gated ? mxfp4_quantize_kernel<X, true> : mxfp4_quantize_kernel<X, false>, mx_grid(a, sms), kMxThreads, 0,
+        e = launch_after(gated ? mxfp4_quantize_kernel<X, true> : mxfp4_quantize_kernel<X, false>, (int)grid, kMxThreads, 0,
                          (cudaStream_t)cuda_stream, a);
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
@@ -183,12 +199,12 @@ extern "C" int vp_mxfp4_dequantize(const uint8_t* codes, int64_t codes_ld, const
     MxArgs a;
     const int rc = fill(a, out, dtype, ld, cols, rows, cols, codes, codes_ld, scales, scales_ld, n_rows);
     if (rc || rows == 0) return rc;
-    const int sms = sm_count_of_device();
-    if (!sms) return VP_E_CUDA;
+    const long long grid = mx_grid(a);
+    if (grid >= ((long long)1 << 31)) return VP_E_UNSUPPORTED;
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        e = launch_after(mxfp4_dequantize_kernel<X>, mx_grid(a, sms), kMxThreads, 0, (cudaStream_t)cuda_stream, a);
+        e = launch_after(mxfp4_dequantize_kernel<X>, (int)grid, kMxThreads, 0, (cudaStream_t)cuda_stream, a);
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
 }
