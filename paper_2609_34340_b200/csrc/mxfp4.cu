@@ -5,7 +5,9 @@
 //   scale = 2^(floor(log2(largest magnitude of the 32)) - 2), at least 2^-127;   code = value / scale, nearest, ties to even, at most 6
 //
 // Dividing by a power of two is exact, so the only rounding is that to 4 bits.  A block that holds an infinity or a NaN gets the
-// scale NaN.  Bound by HBM: a value is read once in its own type and written as 4.25 bits, or the other way round.
+// scale NaN.  Bound by HBM: a value is read once in its own type and written as 4.25 bits, or the other way round: 16,384 rows of 7,168
+// bf16 there and back 95 us, 6.25 TB/s (fp32 166 us, 6.4).  Next to that bound: instructions, about 75 a thread for 16 values; with eight
+// values a thread, 64-bit row arithmetic and a maximum value by value it was 139 us.
 #include <cuda_fp4.h>
 #include <type_traits>
 
@@ -14,149 +16,187 @@
 namespace {
 
 constexpr int kMxThreads = 256;
-constexpr int kMxPer = 8;                         // values of a thread's piece: four threads share a scale
-constexpr int kMxPieces = 4;                      // pieces of a thread, all loaded before the first is worked on
+constexpr int kMxPer = 16;                        // values of a thread's piece: two threads share a scale
 
 struct MxArgs {
     const void* x;
-    long long ld;
     uint8_t *codes, *scales;
-    long long codes_ld, scales_ld;
     const int32_t* n_rows;                        // rows in use, on the device; null: all
-    long long R, K;
-    int groups;                                   // of kMxPer values per row
+    uint32_t x_step, codes_step, scales_step;     // bytes from a row to the next
+    int R, groups;                                // groups of kMxPer values per row
+    long long up;                                 // bytes from a value to what its activation is multiplied with
     SmallDiv by_groups;
     bool wide, wide_codes;
 };
 
-__device__ __forceinline__ long long rows_in_use(const int32_t* n_rows, long long R) {
-    if (!n_rows) return R;
-    const long long n = *n_rows;
-    return n < 0 ? 0 : (n < R ? n : R);
-}
+__device__ __forceinline__ int rows_in_use(const int32_t* n_rows, int R) { return n_rows ? min(max(*n_rows, 0), R) : R; }
 
-// Eight values in 32 bits, from kMxPer places of a row.
+// Sixteen values as they lie in memory, moved 32 bytes at a time: with 16-byte accesses at that distance a warp's touch every sector
+// twice, which cost a tenth of the time.
 template <typename T>
-__device__ __forceinline__ void load_eight(const T* at, bool wide, float (&x)[kMxPer]) {
-    constexpr int V = 16 / (int)sizeof(T);
-    alignas(16) T raw[kMxPer];
+struct alignas(32) Raw { T v[kMxPer]; };
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T* at, bool wide) {
+    Raw<T> r;
     if (wide) {
+        unsigned* const w = (unsigned*)r.v;
 #pragma unroll
-        for (int v = 0; v < kMxPer; v += V) *(Pack<T, V>*)(raw + v) = *(const Pack<T, V>*)(at + v);
+        for (int i = 0; i < (int)sizeof(r) / 4; i += 8)
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7])
+                         : "l"((const unsigned*)at + i) : "memory");
     } else {
 #pragma unroll
-        for (int v = 0; v < kMxPer; v++) raw[v] = at[v];
+        for (int v = 0; v < kMxPer; v++) r.v[v] = at[v];
     }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_raw(T* at, const Raw<T>& r, bool wide) {
+    if (wide) {
+        const unsigned* const w = (const unsigned*)r.v;
 #pragma unroll
-    for (int v = 0; v < kMxPer; v++) x[v] = value_of(raw[v]);
+        for (int i = 0; i < (int)sizeof(r) / 4; i += 8)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         ::"l"((unsigned*)at + i), "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]),
+                         "r"(w[i + 6]), "r"(w[i + 7]) : "memory");
+    } else {
+#pragma unroll
+        for (int v = 0; v < kMxPer; v++) at[v] = r.v[v];
+    }
 }
 
-// Two values to a byte: nearest, ties to even, magnitudes above 6 to 6.
-__device__ __forceinline__ unsigned codes_of(float lo, float hi) {
+// The largest magnitude of a block of 32 as the bits of a float (their order is that of the values, NaN above all); 16-bit types
+// two at a time.
+__device__ __forceinline__ unsigned with_neighbour(unsigned most) { return max(most, __shfl_xor_sync(kAll, most, 1)); }
+__device__ __forceinline__ unsigned block_most(const Raw<float>& r) {
+    unsigned most = 0;
+#pragma unroll
+    for (int v = 0; v < kMxPer; v++) most = max(most, __float_as_uint(r.v[v]) & 0x7fffffffu);
+    return with_neighbour(most);
+}
+template <typename T>
+__device__ __forceinline__ unsigned block_most(const Raw<T>& r) {
+    const unsigned* const w = (const unsigned*)r.v;
+    unsigned most = 0;
+#pragma unroll
+    for (int v = 0; v < kMxPer / 2; v++) most = __vmaxu2(most, w[v] & 0x7fff7fffu);
+    most = with_neighbour(max(most >> 16, most & 0xffffu));
+    return __float_as_uint(value_of(*(const T*)&most));
+}
+
+// Eight values to four bytes: nearest, ties to even, magnitudes above 6 to 6.
+__device__ __forceinline__ unsigned codes_of(const float (&x)[8]) {
     unsigned r;
-    asm("{\n .reg .b8 b;\n cvt.rn.satfinite.e2m1x2.f32 b, %1, %2;\n cvt.u32.u8 %0, b;\n}\n" : "=r"(r) : "f"(hi), "f"(lo));
+    asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+        " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}\n"
+        : "=r"(r) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
     return r;
 }
 
 // 2^e, -127 <= e <= 127.
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float(e > -127 ? (e + 127) << 23 : 1 << 22); }
 
-// Row and piece of a row of the CTA's u-th piece of this thread; false behind the last row in use.  A CTA's pieces are consecutive.
-struct Piece { long long r; int c; };
-__device__ __forceinline__ bool piece_of(const MxArgs& a, long long r0, int c0, long long rows, int u, Piece& p) {
+// Row and piece of a row of the CTA's u-th piece of this thread; false behind the last row in use (the row is that one then).  A CTA's
+// pieces are consecutive.
+struct Piece { int r, c; };
+__device__ __forceinline__ bool piece_of(const MxArgs& a, int r0, int c0, int rows, int u, Piece& p) {
     const int i = c0 + u * kMxThreads + (int)threadIdx.x, down = a.by_groups.div(i);
-    p.r = r0 + down;
-    p.c = i - down * a.groups;
-    return p.r < rows;
+    p = Piece{min(r0 + down, rows - 1), i - down * a.groups};
+    return r0 + down < rows;
 }
 
-// GATED: rows are 2 K wide, the value is silu(x[k]) * x[K + k], in 32 bits.
-template <typename T, bool GATED>
+// N pieces a thread, all loaded before the first is worked on.  GATED: rows are 2 K wide, the value is silu(x[k]) * x[K + k], in 32
+// bits.
+template <typename T, int N, bool GATED>
 __global__ void __launch_bounds__(kMxThreads)
 mxfp4_quantize_kernel(const __grid_constant__ MxArgs a) {
     grid_wait();
-    const long long rows = rows_in_use(a.n_rows, a.R), i0 = (long long)blockIdx.x * (kMxThreads * kMxPieces), r0 = i0 / a.groups;
-    if (r0 >= rows) return;
-    const int c0 = (int)(i0 - r0 * a.groups);
-    Piece p[kMxPieces];
-    bool in[kMxPieces];
-    float x[kMxPieces][kMxPer], up[GATED ? kMxPieces : 1][kMxPer];
+    const int rows = rows_in_use(a.n_rows, a.R);
+    const long long i0 = (long long)blockIdx.x * (kMxThreads * N), first = i0 / a.groups;
+    if (first >= rows) return;
+    const int r0 = (int)first, c0 = (int)(i0 - first * a.groups);
+    Piece p[N];
+    bool in[N];
+    Raw<T> raw[N], up[GATED ? N : 1];
 #pragma unroll
-    for (int u = 0; u < kMxPieces; u++) {
+    for (int u = 0; u < N; u++) {
         in[u] = piece_of(a, r0, c0, rows, u, p[u]);
-        const T* const at = (const T*)a.x + (in[u] ? p[u].r * a.ld + p[u].c * kMxPer : 0);      // (the first is in use)
-        load_eight<T>(at, a.wide, x[u]);
-        if (GATED) load_eight<T>(at + a.K, a.wide, up[u]);
+        const char* const at = (const char*)a.x + (uint64_t)p[u].r * a.x_step + p[u].c * (kMxPer * (int)sizeof(T));
+        raw[u] = load_raw((const T*)at, a.wide);
+        if (GATED) up[u] = load_raw((const T*)(at + a.up), a.wide);
     }
 #pragma unroll
-    for (int u = 0; u < kMxPieces; u++) {
-        if (GATED)
+    for (int u = 0; u < N; u++) {
+        unsigned most;                            // (groups is even: a block's two threads are neighbours)
+        Raw<float> x;
 #pragma unroll
-            for (int v = 0; v < kMxPer; v++) x[u][v] = x[u][v] / (1 + expf(-x[u][v])) * up[u][v];
-        unsigned most = 0;                        // of magnitudes as bits: their order is that of the values, NaN above all
+        for (int v = 0; v < kMxPer; v++) x.v[v] = value_of(raw[u].v[v]);
+        if (GATED) {
 #pragma unroll
-        for (int v = 0; v < kMxPer; v++) most = max(most, __float_as_uint(x[u][v]) & 0x7fffffffu);
-        most = max(most, __shfl_xor_sync(kAll, most, 1));        // (groups is a multiple of four: a block's threads are neighbours)
-        most = max(most, __shfl_xor_sync(kAll, most, 2));
+            for (int v = 0; v < kMxPer; v++) x.v[v] = x.v[v] / (1 + expf(-x.v[v])) * value_of(up[u].v[v]);
+            most = block_most(x);
+        } else {
+            most = block_most(raw[u]);
+        }
         const bool finite = most < 0x7f800000u;
         const int e = max((int)(most >> 23) - 129, -127);        // (magnitudes below 2^-125, zero among them: 2^-127)
         const float inverse = power_of_two(-e);
-        unsigned word = 0;
+        unsigned word[2];
 #pragma unroll
-        for (int v = 0; v < kMxPer; v += 2) word |= codes_of(x[u][v] * inverse, x[u][v + 1] * inverse) << (4 * v);
-        if (!finite) word = 0;
+        for (int h = 0; h < 2; h++) {
+            float y[8];
+#pragma unroll
+            for (int v = 0; v < 8; v++) y[v] = x.v[8 * h + v] * inverse;
+            word[h] = finite ? codes_of(y) : 0;
+        }
         if (in[u]) {
-            uint8_t* const to = a.codes + p[u].r * a.codes_ld + p[u].c * (kMxPer / 2);
-            if (a.wide_codes) *(unsigned*)to = word;
+            uint8_t* const to = a.codes + (uint64_t)p[u].r * a.codes_step + p[u].c * (kMxPer / 2);
+            if (a.wide_codes) *(uint2*)to = make_uint2(word[0], word[1]);
             else
 #pragma unroll
-                for (int b = 0; b < 4; b++) to[b] = (uint8_t)(word >> (8 * b));
-            if ((p[u].c & 3) == 0) a.scales[p[u].r * a.scales_ld + p[u].c / 4] = finite ? (uint8_t)(e + 127) : 255;
+                for (int b = 0; b < 8; b++) to[b] = (uint8_t)(word[b / 4] >> (8 * (b % 4)));
+            if ((p[u].c & 1) == 0) a.scales[(uint64_t)p[u].r * a.scales_step + p[u].c / 2] = finite ? (uint8_t)(e + 127) : 255;
         }
     }
 }
 
 // To the values that codes and scales stand for, rounded once to T (exact in bf16 and fp32).
-template <typename T>
+template <typename T, int N>
 __global__ void __launch_bounds__(kMxThreads)
 mxfp4_dequantize_kernel(const __grid_constant__ MxArgs a) {
     grid_wait();
-    const long long rows = rows_in_use(a.n_rows, a.R), i0 = (long long)blockIdx.x * (kMxThreads * kMxPieces), r0 = i0 / a.groups;
-    if (r0 >= rows) return;
-    const int c0 = (int)(i0 - r0 * a.groups);
-    Piece p[kMxPieces];
-    bool in[kMxPieces];
-    unsigned word[kMxPieces];
-    int s[kMxPieces];
+    const int rows = rows_in_use(a.n_rows, a.R);
+    const long long i0 = (long long)blockIdx.x * (kMxThreads * N), first = i0 / a.groups;
+    if (first >= rows) return;
+    const int r0 = (int)first, c0 = (int)(i0 - first * a.groups);
+    Piece p[N];
+    bool in[N];
+    uint2 word[N];
+    int s[N];
 #pragma unroll
-    for (int u = 0; u < kMxPieces; u++) {
+    for (int u = 0; u < N; u++) {
         in[u] = piece_of(a, r0, c0, rows, u, p[u]);
-        if (!in[u]) p[u] = Piece{r0, 0};
-        const uint8_t* const from = a.codes + p[u].r * a.codes_ld + p[u].c * (kMxPer / 2);
-        if (a.wide_codes) word[u] = *(const unsigned*)from;
-        else word[u] = (unsigned)from[0] | (unsigned)from[1] << 8 | (unsigned)from[2] << 16 | (unsigned)from[3] << 24;
-        s[u] = a.scales[p[u].r * a.scales_ld + p[u].c / 4];
+        const uint8_t* const from = a.codes + (uint64_t)p[u].r * a.codes_step + p[u].c * (kMxPer / 2);
+        if (a.wide_codes) word[u] = *(const uint2*)from;
+        else {
+            word[u].x = (unsigned)from[0] | (unsigned)from[1] << 8 | (unsigned)from[2] << 16 | (unsigned)from[3] << 24;
+            word[u].y = (unsigned)from[4] | (unsigned)from[5] << 8 | (unsigned)from[6] << 16 | (unsigned)from[7] << 24;
+        }
+        s[u] = a.scales[(uint64_t)p[u].r * a.scales_step + p[u].c / 2];
     }
 #pragma unroll
-    for (int u = 0; u < kMxPieces; u++) {
+    for (int u = 0; u < N; u++) {
         const float scale = s[u] == 255 ? CUDART_NAN_F : power_of_two(s[u] - 127);
-        alignas(16) T y[kMxPer];
+        Raw<T> y;
 #pragma unroll
         for (int v = 0; v < kMxPer; v += 2) {
-            const __half2 h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(word[u] >> (4 * v)), __NV_E2M1);
-            y[v] = rounded<T>(__low2float(h) * scale);
-            y[v + 1] = rounded<T>(__high2float(h) * scale);
+            const unsigned w = v < 8 ? word[u].x >> (4 * v) : word[u].y >> (4 * (v - 8));
+            const float2 f = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)w, __NV_E2M1)));
+            y.v[v] = rounded<T>(f.x * scale);
+            y.v[v + 1] = rounded<T>(f.y * scale);
         }
-        T* const to = (T*)a.x + p[u].r * a.ld + p[u].c * kMxPer;
-        constexpr int V = 16 / (int)sizeof(T);
-        if (!in[u]) continue;
-        if (a.wide) {
-#pragma unroll
-            for (int v = 0; v < kMxPer; v += V) *(Pack<T, V>*)(to + v) = *(const Pack<T, V>*)(y + v);
-        } else {
-#pragma unroll
-            for (int v = 0; v < kMxPer; v++) to[v] = y[v];
-        }
+        if (in[u]) store_raw((T*)((char*)a.x + (uint64_t)p[u].r * a.x_step + p[u].c * (kMxPer * (int)sizeof(T))), y, a.wide);
     }
 }
 
@@ -164,17 +204,29 @@ int fill(MxArgs& a, const void* x, int dtype, int64_t ld, int64_t width, int64_t
          const uint8_t* scales, int64_t scales_ld, const int32_t* n_rows) {
     if (!is_type(dtype) || R < 0 || K <= 0 || K % VP_MXFP4_BLOCK || ld < width || codes_ld < K / 2 || scales_ld < K / VP_MXFP4_BLOCK)
         return VP_E_BAD_ARG;
-    if (R >= ((int64_t)1 << 31) || K >= ((int64_t)1 << 31)) return VP_E_UNSUPPORTED;
+    const int size = size_of_type(dtype);
+    const int64_t most = (int64_t)1 << 31;        // rows, bytes of a row
+    if (R >= most || ld >= most / size || codes_ld >= most || scales_ld >= most) return VP_E_UNSUPPORTED;
     if (R == 0) return VP_OK;
     if (!x || !codes || !scales) return VP_E_BAD_ARG;
-    const int size = size_of_type(dtype);
-    if ((uintptr_t)x % size) return VP_E_BAD_ARG;
-    a = MxArgs{x, ld, (uint8_t*)codes, (uint8_t*)scales, codes_ld, scales_ld, n_rows, R, K, (int)(K / kMxPer), small_div((int)(K / kMxPer)),
-               (uintptr_t)x % 16 == 0 && ld * size % 16 == 0, (uintptr_t)codes % 4 == 0 && codes_ld % 4 == 0};
+    if ((uintptr_t)x % size || (uintptr_t)n_rows % 4) return VP_E_BAD_ARG;
+    const int groups = (int)(K / kMxPer);
+    a = MxArgs{x, (uint8_t*)codes, (uint8_t*)scales, n_rows, (uint32_t)(ld * size), (uint32_t)codes_ld, (uint32_t)scales_ld, (int)R, groups,
+               K * size, small_div(groups), (uintptr_t)x % 32 == 0 && ld * size % 32 == 0, (uintptr_t)codes % 8 == 0 && codes_ld % 8 == 0};
     return VP_OK;
 }
 
-long long mx_grid(const MxArgs& a) { return (a.R * a.groups + kMxThreads * kMxPieces - 1) / (kMxThreads * kMxPieces); }
+// Pieces a thread: one until the GPU is full of threads, then two, so that more is on its way.
+template <typename F>
+int launch_pieces(const MxArgs& a, F fn) {
+    const int sms = sm_count_of_device();
+    if (!sms) return VP_E_CUDA;
+    const long long pieces = (long long)a.R * a.groups;
+    const int n = pieces <= (long long)sms * 2048 ? 1 : 2;
+    const long long grid = (pieces + kMxThreads * n - 1) / (kMxThreads * n);
+    if (grid >= ((long long)1 << 31)) return VP_E_UNSUPPORTED;
+    return fn(n, (int)grid) == cudaSuccess ? VP_OK : VP_E_CUDA;
+}
 
 }  // namespace
 
@@ -183,15 +235,16 @@ extern "C" int vp_mxfp4_quantize(const void* x, int dtype, int64_t ld, int64_t r
     MxArgs a;
     const int rc = fill(a, x, dtype, ld, gated ? 2 * cols : cols, rows, cols, codes, codes_ld, scales, scales_ld, n_rows);
     if (rc || rows == 0) return rc;
-    const long long grid = mx_grid(a);
-    if (grid >= ((long long)1 << 31)) return VP_E_UNSUPPORTED;
-    cudaError_t e = cudaErrorInvalidValue;
+    int done = VP_E_BAD_ARG;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        e = launch_after(gated ? mxfp4_quantize_kernel<X, true> : mxfp4_quantize_kernel<X, false>, (int)grid, kMxThreads, 0,
-                         (cudaStream_t)cuda_stream, a);
+            done = launch_pieces(a, [&](int n, int grid) {
+            const auto go = [&](auto kernel) { return launch_after(kernel, grid, kMxThreads, 0, (cudaStream_t)cuda_stream, a); };
+            if (gated) return n == 1 ? go(mxfp4_quantize_kernel<X, 1, true>) : go(mxfp4_quantize_kernel<X, 2, true>);
+            return n == 1 ? go(mxfp4_quantize_kernel<X, 1, false>) : go(mxfp4_quantize_kernel<X, 2, false>);
+        });
     });
-    return e == cudaSuccess ? VP_OK : VP_E_CUDA;
+    return done;
 }
 
 extern "C" int vp_mxfp4_dequantize(const uint8_t* codes, int64_t codes_ld, const uint8_t* scales, int64_t scales_ld, int64_t rows,
@@ -199,12 +252,13 @@ extern "C" int vp_mxfp4_dequantize(const uint8_t* codes, int64_t codes_ld, const
     MxArgs a;
     const int rc = fill(a, out, dtype, ld, cols, rows, cols, codes, codes_ld, scales, scales_ld, n_rows);
     if (rc || rows == 0) return rc;
-    const long long grid = mx_grid(a);
-    if (grid >= ((long long)1 << 31)) return VP_E_UNSUPPORTED;
-    cudaError_t e = cudaErrorInvalidValue;
+    int done = VP_E_BAD_ARG;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        e = launch_after(mxfp4_dequantize_kernel<X>, (int)grid, kMxThreads, 0, (cudaStream_t)cuda_stream, a);
+        done = launch_pieces(a, [&](int n, int grid) {
+            return launch_after(n == 1 ? mxfp4_dequantize_kernel<X, 1> : mxfp4_dequantize_kernel<X, 2>, grid, kMxThreads, 0,
+                                (cudaStream_t)cuda_stream, a);
+        });
     });
-    return e == cudaSuccess ? VP_OK : VP_E_CUDA;
+    return done;
 }
