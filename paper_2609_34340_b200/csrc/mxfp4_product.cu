@@ -6,10 +6,12 @@
 // on the block-scaled tensor-core path (tcgen05.mma, E2M1 operands, an E8M0 scale per 32 values): products are exact, sums are
 // in 32 bits in tensor memory, rounded once to the output's type.
 //
-// One persistent CTA per SM takes output tiles of 128 rows x NT features in turn.  Per 256 values of k a stage of shared memory holds
-// both operands (TMA, 128-byte swizzle) and their scales; warp 0 loads operands, warps 2 and 3 load scales and lay them out as the
-// tensor core reads them, warp 1 issues the copies of scales into tensor memory and the products, warps 4 to 7 bring finished
-// tiles from tensor memory to the output while the next tile is summed.
+// Persistent CTAs take output tiles in turn: one CTA 128 rows x 128 features, or, where there are tiles enough, a pair of CTAs 256 x 256,
+// each holding its own 128 rows and half of the features (cta_group::2), which halves what the features' operand costs in L2
+// traffic.  Per 256 values of k a stage of shared memory holds both operands (TMA, 128-byte swizzle) and their scales; warp 0 loads
+// operands, warps 2, 3 and 8 load scales and lay them out as the tensor core reads them, warp 1 (of the first CTA of a pair) issues the
+// copies of scales into tensor memory and the products, warps 4 to 7 bring finished tiles from tensor memory to the output while the next
+// tile is summed.
 #include <cuda.h>
 #include <type_traits>
 
@@ -23,25 +25,30 @@ constexpr int kPrMaxK = 1 << 20, kPrMaxF = 1 << 20;      // (a matrix is below 2
 constexpr int kPrM = 128;                         // rows of a tile: lanes of tensor memory
 constexpr int kPrK = 256;                         // values of k per stage: one swizzle atom of 128 bytes
 constexpr int kPrBox = 32;                        // rows per TMA box of the rows' operand
-constexpr int kPrThreads = 256;
+constexpr int kPrThreads = 320;
+constexpr int kPrLine = 64;                       // bytes of an output row that leave together
 constexpr unsigned kPrPolls = 1u << 22;
 
-template <int NT>
+// CG: CTAs that share a tile.
+template <int CG>
 struct Shape {
-    static constexpr int stages = NT == 256 ? 4 : 6;
-    static constexpr int a_bytes = kPrM * (kPrK / 2), b_bytes = NT * (kPrK / 2);
-    static constexpr int sa_bytes = kPrM * (kPrK / 32), sb_bytes = NT * (kPrK / 32);
-    static constexpr int stage = a_bytes + b_bytes + sa_bytes + sb_bytes;
-    // Tensor memory, 512 columns.  Scales have a place per stage, so a stage's scales are overwritten only after the products that
-    // read them.  Two tiles of 256 columns and the scales do not fit side by side: the second tile then shares columns with the
-    // first, and a tile is begun as soon as the shared columns of the one before it have been read.
-    static constexpr int scale_cols = 8 + NT / 32 * 2;
-    static constexpr int scales_at = 512 - stages * scale_cols;
-    static constexpr int second_at = NT == 256 ? scales_at - NT : NT;
+    static constexpr int NT = 128 * CG;           // features of a tile
+    static constexpr int b_bytes = 128 * (kPrK / 2), a_bytes = kPrM * (kPrK / 2);           // operands of a stage, per CTA
+    static constexpr int stages = CG == 1 ? 6 : 5, most_stages = CG == 1 ? 8 : 5;
+    static constexpr int operands = stages * (a_bytes + b_bytes);
+    static constexpr int sa_bytes = kPrM * (kPrK / 32), sb_bytes = NT * (kPrK / 32);        // scales (every CTA holds all features')
+    static constexpr int out_bytes = 4 * 32 * kPrLine;                                      // a line of every row of the four warps
+    static constexpr int scales_begin = operands, out_begin = scales_begin + most_stages * (sa_bytes + sb_bytes),
+                         lists_begin = out_begin + out_bytes;
+    // Tensor memory, 512 columns.  Scales have a place per stage, so a stage's are copied over those of products that are done.  Two tiles of 256 columns and the scales do not fit side by side: the second tile
+    // then shares columns with the first, and a tile is begun as soon as the shared columns of the one before it have been read.
+    static constexpr int scale_cols = 8 + NT / 32 * 2, scale_places = most_stages;
+    static constexpr int scales_at = 512 - scale_places * scale_cols;
+    static constexpr int second_at = 128;
     static constexpr bool shared_cols = second_at < NT;
     static constexpr int lag = shared_cols ? 1 : 2;
-    static constexpr int first_chunks = shared_cols ? (NT - second_at) / 32 : NT / 32;     // of 32 columns: read before the next tile
-    static_assert(scales_at >= second_at + NT && (NT - second_at) % 32 == 0, "columns of tensor memory");
+    static constexpr int first_chunks = shared_cols ? (NT - second_at) / 32 : NT / 32;      // of 32 columns: read before the next tile
+    static_assert(scales_at >= second_at + NT && first_chunks == 4, "columns of tensor memory");
 };
 
 struct ProductArgs {
@@ -55,35 +62,76 @@ struct ProductArgs {
     int32_t* status;
 };
 
-__device__ __forceinline__ void mbar_arrive(unsigned bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+// An address of this CTA's shared memory in the CTA of that rank of the cluster.
+__device__ __forceinline__ unsigned in_cta(unsigned at, unsigned rank) {
+    unsigned r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(rank));
+    return r;
 }
+__device__ __forceinline__ void cluster_arrive(unsigned bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_expect_tx(unsigned bar, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
+}
+// Boxes of a tensor map into this CTA's shared memory (no multicast); the barrier may be the pair's first CTA's.
+template <int CG>
 __device__ __forceinline__ void tma_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+    if constexpr (CG == 1)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+template <int CG>
 __device__ __forceinline__ void tma_3d(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    if constexpr (CG == 1)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 // Shared-memory operand descriptors: 128-byte swizzle, rows of 128 bytes in groups of eight; and plain rows of 16 bytes for scales.
-__device__ __forceinline__ uint64_t operand_desc(unsigned at) {
-    return (uint64_t)(at >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+constexpr uint64_t kOperandDesc = (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+constexpr uint64_t kScaleDesc = (uint64_t)(128 >> 4) << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+__device__ __forceinline__ uint64_t desc_of(uint64_t kind, unsigned at16) { return kind | at16; }     // at16: the address over 16
+__device__ __forceinline__ bool elect_one() {
+    unsigned r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r != 0;
 }
-__device__ __forceinline__ uint64_t scale_desc(unsigned at) {
-    return (uint64_t)(at >> 4) | (uint64_t)(128 >> 4) << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
-}
+// Per CTA of the pair: its own shared memory to its own tensor memory.
+template <int CG>
 __device__ __forceinline__ void copy_scales(unsigned tmem, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
+template <int CG>
 __device__ __forceinline__ void mma_mxf4(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned sa, unsigned sb, bool add) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((unsigned)add) : "memory");
+    if constexpr (CG == 1)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+            ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((unsigned)add) : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+            ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((unsigned)add) : "memory");
 }
+// One arrival at the barrier (of both CTAs of a pair) when everything issued so far is done.
+template <int CG>
 __device__ __forceinline__ void mma_commit(unsigned bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -100,97 +148,131 @@ __device__ __forceinline__ void load_columns(unsigned tmem, unsigned (&r)[32]) {
         : "r"(tmem) : "memory");
 }
 
-// The experts that have rows, in order: id, first row, rows, and the row tiles in front of them.
+// The experts that have rows, in order: id, and the row tiles in front of them.
 struct Experts {
-    int *id, *first, *rows, *tiles;               // tiles: one entry more
+    int* tiles;                                   // one entry more
+    uint16_t* id;
     int n;
 };
 
+// Rows of an expert; offsets are held inside the buffer whatever they are.
+struct Rows { int first, n; };
+__device__ __forceinline__ Rows rows_of(const ProductArgs& a, int e, bool& bad) {
+    const int lo = a.off[e], hi = a.off[e + 1], first = min(max(lo, 0), a.R);
+    bad = lo < 0 || hi < lo || hi > a.R;
+    return Rows{first, max(min(max(hi, 0), a.R) - first, 0)};
+}
+
 struct Tile {
-    int e, first, rows, n0;                       // expert, first row, rows (at most kPrM), first feature
+    int e, first, rows, n0;                       // expert, first row, rows (at most mt), first feature
 };
 
-__device__ __forceinline__ Tile tile_of(const Experts& x, long long tile, int n_tiles, int nt) {
+__device__ __forceinline__ Tile tile_of(const ProductArgs& a, const Experts& x, long long tile, int n_tiles, int mt, int nt) {
     // tiles of an expert: its row tiles next to one another, feature tile by feature tile
     int lo = 0, hi = x.n - 1;
     while (lo < hi) {                             // the last expert whose first tile is not behind `tile`
         const int mid = (lo + hi + 1) / 2;
         if ((long long)x.tiles[mid] * n_tiles <= tile) lo = mid; else hi = mid - 1;
     }
+    bool bad;
+    const Rows r = rows_of(a, x.id[lo], bad);
     const int m_tiles = x.tiles[lo + 1] - x.tiles[lo];
     const int q = (int)(tile - (long long)x.tiles[lo] * n_tiles), m = q % m_tiles;
-    return Tile{x.id[lo], x.first[lo] + m * kPrM, min(kPrM, x.rows[lo] - m * kPrM), q / m_tiles * nt};
+    return Tile{x.id[lo], r.first + m * mt, min(mt, r.n - m * mt), q / m_tiles * nt};
 }
 
-// 16 bytes of scales from byte k of a row of `bytes`; 1 behind its end and in rows that are not there.
-__device__ __forceinline__ uint4 load_scales(const uint8_t* row, int k, int bytes, bool there) {
-    uint4 v = make_uint4(0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f);
-    if (!there || k >= bytes) return v;
+// 32 scales from byte k of a row of `bytes`; 1 behind its end and in rows that are not there.
+struct alignas(16) Scales { unsigned w[8]; };
+__device__ __forceinline__ Scales load_scales(const uint8_t* row, int k, int bytes, bool there) {
+    Scales v;
     const uint8_t* const p = row + k;
-    if (k + 16 <= bytes && ((uintptr_t)p & 15) == 0) return *(const uint4*)p;
-    unsigned* const w = (unsigned*)&v;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        if (k + 4 * i + 4 <= bytes && ((uintptr_t)p & 3) == 0) w[i] = *(const unsigned*)(p + 4 * i);
-        else
-#pragma unroll
-            for (int b = 0; b < 4; b++)
-                if (k + 4 * i + b < bytes) w[i] = (w[i] & ~(255u << (8 * b))) | (unsigned)p[4 * i + b] << (8 * b);
+    if (there && k + 32 <= bytes && ((uintptr_t)p & 31) == 0) {       // a sector at once: every part of it is a request to L2 of its own
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7]) : "l"(p));
+        return v;
     }
+#pragma unroll
+    for (int i = 0; i < 8; i++) v.w[i] = 0x7f7f7f7f;
+    if (!there) return v;
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+        if (k + 16 * h + 16 <= bytes && ((uintptr_t)p & 15) == 0) {
+            *(uint4*)(v.w + 4 * h) = *(const uint4*)(p + 16 * h);
+        } else {
+#pragma unroll
+            for (int i = 4 * h; i < 4 * h + 4; i++) {
+                if (k + 4 * i + 4 <= bytes && ((uintptr_t)p & 3) == 0) v.w[i] = *(const unsigned*)(p + 4 * i);
+                else
+#pragma unroll
+                    for (int b = 0; b < 4; b++)
+                        if (k + 4 * i + b < bytes) v.w[i] = (v.w[i] & ~(255u << (8 * b))) | (unsigned)p[4 * i + b] << (8 * b);
+            }
+        }
     return v;
 }
 
-template <int NT, typename T>
+template <int CG, typename T>
 __global__ void __launch_bounds__(kPrThreads, 1)
 mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map,
                      const __grid_constant__ ProductArgs a) {
-    using S = Shape<NT>;
+    using S = Shape<CG>;
+    constexpr int NT = S::NT, MT = kPrM * CG;
     extern __shared__ unsigned char s_raw[];
-    __shared__ uint64_t s_bar[2 * S::stages + 5];
+    __shared__ uint64_t s_bar[3 * S::most_stages + 5];
     __shared__ unsigned s_tmem;
-    __shared__ int s_n;
+    __shared__ int s_n, s_most;
     __shared__ volatile int s_stop;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = CG == 1 ? 0 : (int)(blockIdx.x % CG);          // of the pair
     const unsigned base = (smem_u32(s_raw) + 1023) & ~1023u;
-    int* const lists = (int*)(s_raw + (base - smem_u32(s_raw)) + S::stages * S::stage);
-    Experts ex{lists, lists + a.E, lists + 2 * a.E, lists + 3 * a.E, 0};
+    int* const lists = (int*)(s_raw + (base - smem_u32(s_raw)) + S::lists_begin);
+    Experts ex{lists, (uint16_t*)(lists + a.E + 1), 0};
     const unsigned bars = smem_u32(s_bar);
-    const auto full = [&](int s) { return bars + 8 * s; };
-    const auto empty = [&](int s) { return bars + 8 * (S::stages + s); };
-    const auto done = [&](int b) { return bars + 8 * (2 * S::stages + b); };            // a tile is summed
-    const auto free_ = [&](int b) { return bars + 8 * (2 * S::stages + 2 + b); };       // its columns may be used again
-    const unsigned drained = bars + 8 * (2 * S::stages + 4);
+    const auto first_cta = [&](unsigned bar) { return CG == 1 ? bar : in_cta(bar, 0); };
+    const auto full = [&](int s) { return bars + 8 * s; };                                  // of the first CTA: what a stage needs is there
+    const auto empty = [&](int s) { return bars + 8 * (S::most_stages + s); };              // of each: a stage has been read
+    const auto written = [&](int s) { return bars + 8 * (2 * S::most_stages + s); };        // of each: a stage's scales are written
+    const unsigned bars3 = bars + 24 * S::most_stages;
+    const auto done = [&](int b) { return bars3 + 8 * b; };                                 // of each: a tile is summed
+    const auto free_ = [&](int b) { return bars3 + 8 * (2 + b); };                          // of the first: its columns may be used again
+    const unsigned drained = bars3 + 32;
     if (tid == 0) {
-        for (int s = 0; s < S::stages; s++) {
-            mbar_init(full(s), 3);                // the operands' loader and two warps of scales
+        for (int s = 0; s < S::most_stages; s++) {
+            mbar_init(full(s), 2 * CG);           // per CTA: the operands' loader, and warp 9 for the scales
             mbar_init(empty(s), 1);
+            mbar_init(written(s), 1 + CG);
         }
         for (int b = 0; b < 2; b++) {
             mbar_init(done(b), 1);
-            mbar_init(free_(b), 4);
+            mbar_init(free_(b), 4 * CG);
         }
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_stop = 0;
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if constexpr (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        }
     }
     grid_wait();
-    if (warp == 0) {                              // experts with rows; offsets are held inside the buffer whatever they are
-        int n = 0, tiles = 0;
+    if (warp == 0) {                              // experts with rows
+        int n = 0, tiles = 0, most = 0;
         bool bad = false;
         for (int e0 = 0; e0 < a.E; e0 += 32) {
             const int e = e0 + lane;
-            int first = 0, rows = 0;
+            int rows = 0;
             if (e < a.E) {
-                const int lo = a.off[e], hi = a.off[e + 1];
-                bad |= lo < 0 || hi < lo || hi > a.R;
-                first = min(max(lo, 0), a.R);
-                rows = max(min(max(hi, 0), a.R) - first, 0);
+                bool wrong;
+                rows = rows_of(a, e, wrong).n;
+                bad |= wrong;
             }
-            int sum = (rows + kPrM - 1) / kPrM;
+            most = max(most, rows);
+            int sum = (rows + MT - 1) / MT;
             const int own = sum;
             for (int o = 1; o < 32; o *= 2) {
                 const int other = __shfl_up_sync(kAll, sum, o);
@@ -199,28 +281,29 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
             const unsigned who = __ballot_sync(kAll, rows > 0);
             if (rows > 0) {
                 const int at = n + __popc(who & ((1u << lane) - 1));
-                ex.id[at] = e;
-                ex.first[at] = first;
-                ex.rows[at] = rows;
+                ex.id[at] = (uint16_t)e;
                 ex.tiles[at] = tiles + sum - own;
             }
             n += __popc(who);
             tiles += __shfl_sync(kAll, sum, 31);
         }
+        most = __reduce_max_sync(kAll, most);
         if (lane == 0) {
             ex.tiles[n] = tiles;
             s_n = n;
+            s_most = most;
         }
         if (bad && blockIdx.x == 0) atomicOr(a.status, VP_ST_PACK_MISMATCH);
     }
     fence_before();
     __syncthreads();
+    if constexpr (CG > 1) cluster_sync();         // (the other CTA's barriers are there)
     fence_after();
     ex.n = s_n;
     const unsigned tmem = s_tmem;
     const int n_tiles = (a.F + NT - 1) / NT, k_tiles = (a.K + kPrK - 1) / kPrK;
-    const long long tiles = (long long)ex.tiles[ex.n] * n_tiles;
-    // Every wait is bounded: the one that gives up sets the flag, which ends the others'.
+    const long long tiles = (long long)ex.tiles[ex.n] * n_tiles, t0 = blockIdx.x / CG, step = gridDim.x / CG;
+    // Every wait is bounded: the one that gives up sets the flag, which ends the others' (of the other CTA by their own limits).
     const auto wait = [&](unsigned bar, unsigned parity) {
         for (unsigned i = 0; i < kPrPolls; i++) {
             if (mbar_try_wait(bar, parity)) return true;
@@ -230,181 +313,230 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
         atomicOr(a.status, VP_ST_INTERNAL_TIMEOUT);
         return false;
     };
-    int s = 0;
-    unsigned phase = 0;
-    const auto next_stage = [&] { if (++s == S::stages) { s = 0; phase ^= 1; } };
-    const auto a_at = [&](int st) { return base + st * S::stage; };
+    // One CTA: where no expert has more than 32, 64 or 96 rows, a stage holds that many, and there are more stages (the products read 128
+    // rows all the same: what lies behind, any bits being numbers, makes rows that nobody stores).
+    const int a_bytes = CG == 1 ? min((s_most + kPrBox - 1) / kPrBox * kPrBox * (kPrK / 2), S::a_bytes) : S::a_bytes;
+    const int stages = CG == 1 ? min(S::operands / max(a_bytes + S::b_bytes, 1), S::most_stages) : S::stages;
+    struct Ring {                                 // a place of a ring of barriers, and the parity of its turn
+        int at;
+        unsigned phase;
+        __device__ __forceinline__ void next(int n) { if (++at == n) { at = 0; phase ^= 1; } }
+    };
+    Ring s{0, 0};
+    const auto stage_at = [&](int st) { return base + st * (a_bytes + S::b_bytes); };
+    const auto scales_at = [&](int st) { return base + S::scales_begin + st * (S::sa_bytes + S::sb_bytes); };
 
     if (warp == 0) {
         if (lane == 0) {
             bool ok = true;
-            for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-                const Tile tile = tile_of(ex, t, n_tiles, NT);
-                const int boxes = (tile.rows + kPrBox - 1) / kPrBox;
+            for (long long t = t0; ok && t < tiles; t += step) {
+                const Tile tile = tile_of(a, ex, t, n_tiles, MT, NT);
+                const int rows = min(max(tile.rows - rank * kPrM, 0), kPrM), boxes = (rows + kPrBox - 1) / kPrBox;
                 for (int k = 0; k < k_tiles; k++) {
-                    if (!(ok = wait(empty(s), phase ^ 1))) break;
-                    const unsigned at = a_at(s);
-                    mbar_expect_tx(full(s), boxes * kPrBox * (kPrK / 2) + S::b_bytes);
+                    if (!(ok = wait(empty(s.at), s.phase ^ 1))) break;
+                    const unsigned at = stage_at(s.at), bar = first_cta(full(s.at)), bytes = boxes * kPrBox * (kPrK / 2) + S::b_bytes;
+                    if (CG == 1) mbar_expect_tx(bar, bytes);
+                    else cluster_expect_tx(bar, bytes);
+                    tma_3d<CG>(at + a_bytes, &w_map, k * (kPrK / 2), tile.n0 + rank * 128, tile.e, bar);
                     for (int b = 0; b < boxes; b++)
-                        tma_2d(at + b * kPrBox * (kPrK / 2), &x_map, k * (kPrK / 2), tile.first + b * kPrBox, full(s));
-                    tma_3d(at + S::a_bytes, &w_map, k * (kPrK / 2), tile.n0, tile.e, full(s));
-                    next_stage();
+                        tma_2d<CG>(at + b * kPrBox * (kPrK / 2), &x_map, k * (kPrK / 2), tile.first + rank * kPrM + b * kPrBox, bar);
+                    s.next(stages);
                 }
+            }
+            // The pair's first CTA arrives at this one's barriers until the last stage has been read.
+            for (int i = 0; CG > 1 && ok && i < stages; i++) {
+                ok = wait(empty(s.at), s.phase ^ 1);
+                s.next(stages);
             }
             if (!ok)                              // copies that are still on their way (bounded as well)
-                for (int i = 0; i < S::stages; i++) mbar_wait_bounded(full(i), i < s ? phase : phase ^ 1, 1u << 16);
+                for (int i = 0; i < stages; i++) mbar_wait_bounded(full(i), i < s.at ? s.phase : s.phase ^ 1, 1u << 16);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr unsigned idesc = 1u << 7 | 1u << 10 | (unsigned)(NT >> 3) << 17 | 1u << 23 | (unsigned)(kPrM >> 7) << 27;
+        // The whole warp goes along, so that what the instructions take is the same in all lanes and known to be; one lane issues them.
+        if (rank == 0) {
+            constexpr unsigned idesc = 1u << 7 | 1u << 10 | (unsigned)(NT >> 3) << 17 | 1u << 23 | (unsigned)(MT >> 7) << 27;
+            const unsigned tm = __reduce_max_sync(kAll, tmem), rows_bytes = __reduce_max_sync(kAll, (unsigned)a_bytes),
+                           b16 = __reduce_max_sync(kAll, base) >> 4, n_stages = __reduce_max_sync(kAll, (unsigned)stages),
+                           stage16 = (rows_bytes + S::b_bytes) >> 4;
+            const int my_tiles = __reduce_max_sync(kAll, t0 < tiles ? (int)((tiles - 1 - t0) / step) + 1 : 0);
+            const bool one = elect_one();
             bool ok = true;
-            int j = 0;
-            for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x, j++) {
-                if (j >= S::lag && !(ok = wait(free_((j - S::lag) & 1), ((j - S::lag) >> 1) & 1))) break;
+            unsigned st = 0, parity = 0;
+            for (int j = 0; ok && j < my_tiles; j++) {
+                if (j >= S::lag && !(ok = __all_sync(kAll, wait(free_((j - S::lag) & 1), ((j - S::lag) >> 1) & 1)))) break;
                 fence_after();
-                const unsigned d = tmem + (j & 1 ? S::second_at : 0);
+                const unsigned d = tm + (j & 1 ? S::second_at : 0);
                 for (int k = 0; k < k_tiles; k++) {
-                    if (!(ok = wait(full(s), phase))) break;
+                    if (!(ok = __all_sync(kAll, wait(full(st), parity)))) break;
                     fence_after();
-                    const unsigned at = a_at(s), sa = at + S::a_bytes + S::b_bytes, sb = sa + S::sa_bytes;
-                    const unsigned ta = tmem + S::scales_at + s * S::scale_cols, tb = ta + 8;
+                    const unsigned at16 = b16 + st * stage16, sa16 = b16 + (S::scales_begin + st * (S::sa_bytes + S::sb_bytes)) / 16;
+                    const unsigned ta = tm + S::scales_at + st * S::scale_cols, tb = ta + 8;
+                    if (one) {
 #pragma unroll
-                    for (int c = 0; c < 2; c++) copy_scales(ta + 4 * c, scale_desc(sa + 512 * c));
+                        for (int c = 0; c < 2; c++) copy_scales<CG>(ta + 4 * c, desc_of(kScaleDesc, sa16 + 32 * c));
 #pragma unroll
-                    for (int c = 0; c < NT / 64; c++) copy_scales(tb + 4 * c, scale_desc(sb + 512 * c));
+                        for (int c = 0; c < NT / 64; c++) copy_scales<CG>(tb + 4 * c, desc_of(kScaleDesc, sa16 + S::sa_bytes / 16 + 32 * c));
 #pragma unroll
-                    for (int u = 0; u < 4; u++) {       // 64 values of k each; two of a word's four scales
-                        const unsigned half = (u & 1) * 2;
-                        mma_mxf4(d, operand_desc(at + 32 * u), operand_desc(at + S::a_bytes + 32 * u), idesc | half << 29 | half << 4,
-                                 ta + 4 * (u / 2), tb + NT / 32 * (u / 2), k > 0 || u > 0);
+                        for (int u = 0; u < 4; u++) {         // 64 values of k each; two of a word's four scales
+                            const unsigned half = (u & 1) * 2;
+                            mma_mxf4<CG>(d, desc_of(kOperandDesc, at16 + 2 * u), desc_of(kOperandDesc, at16 + (rows_bytes >> 4) + 2 * u),
+                                         idesc | half << 29 | half << 4, ta + 4 * (u / 2), tb + NT / 32 * (u / 2), k > 0 || u > 0);
+                        }
+                        mma_commit<CG>(empty(st));
                     }
-                    mma_commit(empty(s));
-                    next_stage();
+                    __syncwarp();
+                    if (++st == n_stages) { st = 0; parity ^= 1; }
                 }
-                if (ok) mma_commit(done(j & 1));
+                if (ok && one) mma_commit<CG>(done(j & 1));
+                __syncwarp();
             }
-            if (!ok) {                            // products that are still running
-                mma_commit(drained);
+            if (!ok && one) {                     // products that are still running
+                mma_commit<CG>(drained);
                 mbar_wait_bounded(drained, 0, 1u << 16);
             }
         }
-    } else if (warp < 4) {
-        // Scales: row lane + 32 j of the tile is word j of lane's 16 bytes; per 128 values of k and 128 rows 512 bytes.
-        const bool is_b = warp == 3;
-        constexpr int kMost = NT / 32 > 4 ? NT / 32 : 4;
-        const int count = is_b ? NT / 32 : 4, bytes = a.K / 32;
-        const auto load = [&](const Tile& tile, int chunk, uint4 (&v)[kMost][2]) {
+    } else if (warp < 4 || (warp == 8 && CG == 2)) {
+        // Scales of 128 rows or features: row lane + 32 j is word j of lane's 16 bytes, 512 bytes per 128 values of k.  Stages go by
+        // chunks of four (32 scales of a row); the next chunk is on its way while one is handed out.
+        const bool is_b = warp != 2;
+        const int half = warp == 8 ? 1 : 0, bytes = a.K / 32, chunks = (k_tiles + 3) / 4;
+        const unsigned to = (is_b ? S::sa_bytes + 512 * half : 0) + lane * 16, word_step = is_b ? 512 * CG : 512;
+        Tile tile{};
+        const auto load = [&](long long t, int chunk, Scales (&v)[4]) {
+            if (t >= tiles) return;
+            if (chunk == 0) tile = tile_of(a, ex, t, n_tiles, MT, NT);
 #pragma unroll
-            for (int j = 0; j < kMost; j++) {
-                if (j >= count) break;
-                const int r = lane + 32 * j;
+            for (int j = 0; j < 4; j++) {
+                const int r = lane + 32 * j + (is_b ? 128 * half : kPrM * rank);
                 const bool there = is_b ? tile.n0 + r < a.F : r < tile.rows;
                 const uint8_t* const row = is_b ? a.ws + ((long long)tile.e * a.F + tile.n0 + r) * bytes
                                                 : a.xs + (long long)(tile.first + r) * a.xs_ld;
-                v[j][0] = load_scales(row, chunk * 32, bytes, there);
-                v[j][1] = load_scales(row, chunk * 32 + 16, bytes, there);
+                v[j] = load_scales(row, chunk * 32, bytes, there);
             }
         };
-        const int chunks = (k_tiles + 3) / 4;     // of four stages: 32 scales of a row, the next ones on their way
-        uint4 next[kMost][2], now[kMost][2];
-        long long t = blockIdx.x;
-        Tile tile{};
-        if (t < tiles) {
-            tile = tile_of(ex, t, n_tiles, NT);
-            load(tile, 0, next);
-        }
+        Scales next[4], v[4];
+        load(t0, 0, next);
         bool ok = true;
+        long long t = t0;
         for (int chunk = 0; ok && t < tiles;) {
 #pragma unroll
-            for (int j = 0; j < kMost; j++) { now[j][0] = next[j][0]; now[j][1] = next[j][1]; }
+            for (int j = 0; j < 4; j++) v[j] = next[j];
             const int k0 = chunk * 4;
-            if (++chunk == chunks) {
-                chunk = 0;
-                t += gridDim.x;
-                if (t < tiles) tile = tile_of(ex, t, n_tiles, NT);
-            }
-            if (t < tiles) load(tile, chunk, next);
+            if (++chunk == chunks) { chunk = 0; t += step; }
+            load(t, chunk, next);
 #pragma unroll
             for (int k = 0; k < 4; k++) {
                 if (k0 + k >= k_tiles) break;
-                if (!(ok = __all_sync(kAll, wait(empty(s), phase ^ 1)))) break;
-                const unsigned at = a_at(s) + S::a_bytes + S::b_bytes + (is_b ? S::sa_bytes : 0) + lane * 16;
-                const int blocks = count / 4;
+                if (!(ok = __all_sync(kAll, wait(empty(s.at), s.phase ^ 1)))) break;
+                const unsigned at = scales_at(s.at) + to;
 #pragma unroll
-                for (int c = 0; c < kMost / 4; c++) {
-                    if (c >= blocks) break;
-#pragma unroll
-                    for (int w = 0; w < 2; w++) {       // words 2 k + w of the rows' 32 bytes
-                        const int i = 2 * k + w;
-                        const auto word = [&](int j) {
-                            const uint4& q = now[4 * c + j][i / 4];
-                            return i % 4 == 0 ? q.x : (i % 4 == 1 ? q.y : (i % 4 == 2 ? q.z : q.w));
-                        };
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 512 * (w * blocks + c)), "r"(word(0)), "r"(word(1)),
-                                     "r"(word(2)), "r"(word(3)) : "memory");
-                    }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                for (int w = 0; w < 2; w++)               // words 2 k + w of the rows' 32 bytes
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + word_step * w), "r"(v[0].w[2 * k + w]),
+                                 "r"(v[1].w[2 * k + w]), "r"(v[2].w[2 * k + w]), "r"(v[3].w[2 * k + w]) : "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(full(s));
-                next_stage();
+                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(written(s.at)) : "memory");
+                s.next(stages);
             }
         }
-    } else {
+    } else if (warp == 9) {
+        // Makes scales that are written visible to the tensor core's copies.  The fence is a warp's own that has no loads on their way: in the
+        // warps that load scales it waits for those.
+        if (lane == 0) {
+            bool ok = true;
+            for (long long t = t0; ok && t < tiles; t += step)
+                for (int k = 0; k < k_tiles; k++) {
+                    if (!(ok = wait(written(s.at), s.phase))) break;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full(s.at)) : "memory");
+                    else cluster_arrive(first_cta(full(s.at)));
+                    s.next(stages);
+                }
+        }
+    } else if (warp < 8) {
         const int quarter = warp - 4;             // lanes 32 * quarter .. of tensor memory: rows of the tile
+        constexpr int V = 16 / (int)sizeof(T), cols = kPrLine / (int)sizeof(T), per = 32 / cols;        // columns of a line, lines of 32 columns
+        const long long row_bytes = a.out_ld * (long long)sizeof(T);
+        const unsigned stage = base + S::out_begin + quarter * 32 * kPrLine;
         bool ok = true;
         int j = 0;
-        for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x, j++) {
-            const Tile tile = tile_of(ex, t, n_tiles, NT);
-            const int r = quarter * 32 + lane;
-            T* const row = (T*)a.out + (long long)(tile.first + r) * a.out_ld + tile.n0;
-            const bool there = r < tile.rows;
+        for (long long t = t0; ok && t < tiles; t += step, j++) {
+            const Tile tile = tile_of(a, ex, t, n_tiles, MT, NT);
+            const int rows = tile.rows - rank * kPrM - quarter * 32;        // of this warp (or fewer than none)
+            T* const out = (T*)a.out + (long long)(tile.first + rank * kPrM + quarter * 32) * a.out_ld;
             if (!(ok = __all_sync(kAll, wait(done(j & 1), (j >> 1) & 1)))) break;
             fence_after();
             const unsigned from = tmem + ((unsigned)(quarter * 32) << 16) + (j & 1 ? S::second_at : 0);
-            const auto store = [&](const unsigned (&v)[32], int c) {
-                if (!there) return;
-                constexpr int V = 16 / (int)sizeof(T);
-                if (a.out_wide && tile.n0 + c * 32 + 32 <= a.F) {
+            // A line of each of the warp's rows: 16-byte pieces to shared memory (piece p of row r at p ^ r / 2 % 4: no bank twice), then
+            // eight rows at a time to the output.
+            const auto store = [&](const unsigned (*v)[32], int line) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += V) {
-                        Pack<T, V> p;
+                for (int p = 0; p < 4; p++) {
+                    Pack<T, V> q;
 #pragma unroll
-                        for (int u = 0; u < V; u++) p.v[u] = rounded<T>(__uint_as_float(v[i + u]));
-                        *(Pack<T, V>*)(row + c * 32 + i) = p;
-                    }
+                    for (int u = 0; u < V; u++) q.v[u] = rounded<T>(__uint_as_float(v[0][(line * cols + p * V + u) % 32]));
+                    const uint4 w = *(const uint4*)&q;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * kPrLine + ((p ^ (lane >> 1 & 3)) << 4)), "r"(w.x),
+                                 "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+                }
+                __syncwarp();
+                const int c = tile.n0 + line * cols + (lane & 3) * V, r0 = lane >> 2;
+                uint4 w[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i].x), "=r"(w[i].y), "=r"(w[i].z), "=r"(w[i].w)
+                                 : "r"(stage + (8 * i + r0) * kPrLine + (((lane & 3) ^ (r0 >> 1 & 3)) << 4)) : "memory");
+                char* to = (char*)(out + c) + r0 * row_bytes;
+                if (a.out_wide && c + V <= a.F) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++, to += 8 * row_bytes)
+                        if (8 * i + r0 < rows) *(uint4*)to = w[i];
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 32; i++)
-                        if (tile.n0 + c * 32 + i < a.F) row[c * 32 + i] = rounded<T>(__uint_as_float(v[i]));
+                    for (int i = 0; i < 4; i++, to += 8 * row_bytes) {
+                        const Pack<T, V> q = *(const Pack<T, V>*)&w[i];
+#pragma unroll
+                        for (int u = 0; u < V; u++)
+                            if (8 * i + r0 < rows && c + u < a.F) ((T*)to)[u] = q.v[u];
+                    }
                 }
+                __syncwarp();
             };
             // the columns that the next tile waits for first
             const int c0 = S::shared_cols && (j & 1) == 0 ? S::second_at / 32 : 0;
-            unsigned v[S::first_chunks][32];
+            unsigned v[4][32];
 #pragma unroll
-            for (int c = 0; c < S::first_chunks; c++) load_columns(from + 32 * (c0 + c), v[c]);
+            for (int c = 0; c < 4; c++) load_columns(from + 32 * (c0 + c), v[c]);
             wait_loads();
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(free_(j & 1));
+            if (lane == 0) {
+                if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(free_(j & 1)) : "memory");
+                else cluster_arrive(first_cta(free_(j & 1)));
+            }
+            if (rows > 0)
 #pragma unroll
-            for (int c = 0; c < S::first_chunks; c++) store(v[c], c0 + c);
-#pragma unroll 1
-            for (int c = S::first_chunks; c < NT / 32; c++) {
-                const int at = (c0 + c) % (NT / 32);
-                load_columns(from + 32 * at, v[0]);
+                for (int c = 0; c < 4 * per; c++)
+                    if (tile.n0 + (c0 * per + c) * cols < a.F) store(&v[c / per], c0 * per + c);
+            if (NT > 128) {
+                const int c1 = c0 ^ 4;
+#pragma unroll
+                for (int c = 0; c < 4; c++) load_columns(from + 32 * (c1 + c), v[c]);
                 wait_loads();
-                store(v[0], at);
+                if (rows > 0)
+#pragma unroll
+                    for (int c = 0; c < 4 * per; c++)
+                        if (tile.n0 + (c1 * per + c) * cols < a.F) store(&v[c / per], c1 * per + c);
             }
         }
         fence_before();
     }
     __syncwarp();
     __syncthreads();
+    if constexpr (CG > 1) cluster_sync();         // (nobody leaves while its memory is read or its barriers are arrived at)
     if (warp == 1) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+        if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
 }
 
@@ -435,8 +567,29 @@ bool make_map(CUtensorMap* map, int rank, const void* p, const cuuint64_t* dims,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int NT>
-size_t product_smem(int E) { return (size_t)Shape<NT>::stages * Shape<NT>::stage + 1024 + (size_t)(4 * E + 1) * 4; }
+template <int CG>
+size_t product_smem(int E) { return (size_t)Shape<CG>::lists_begin + 1024 + (size_t)E * 6 + 4; }
+
+template <int CG, typename T>
+cudaError_t launch_product(const CUtensorMap& x_map, const CUtensorMap& w_map, const ProductArgs& a, int grid, cudaStream_t stream) {
+    const auto fn = mxfp4_product_kernel<CG, T>;
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)product_smem<CG>(kPrMaxExperts));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kPrThreads);
+    cfg.dynamicSmemBytes = product_smem<CG>(a.E);
+    cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CG; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = CG > 1 ? 2 : 1;
+    g_vp_launches++;
+    return cudaLaunchKernelEx(&cfg, fn, x_map, w_map, a);
+}
 
 }  // namespace
 
@@ -458,25 +611,24 @@ extern "C" int vp_mxfp4_product(const uint8_t* x_codes, int64_t x_codes_ld, cons
     const ProductArgs a{x_scales, w_scales, x_scales_ld, expert_off, E, (int)capacity_rows, (int)F, (int)K, out, out_ld,
                         (uintptr_t)out % 16 == 0 && out_ld * size % 16 == 0, status};
     // Row tiles there can be at most: a part of one per expert more than the rows fill.
-    const long long most = (capacity_rows + kPrM - 1) / kPrM + (E < capacity_rows ? E : capacity_rows);
-    const bool large = most * ((F + 255) / 256) >= 2 * sms;
-    const long long tiles = most * ((F + (large ? 255 : 127)) / (large ? 256 : 128));
-    const int grid = (int)(tiles < sms ? tiles : sms);
+    const auto most_tiles = [&](int mt, int nt) { return ((capacity_rows + mt - 1) / mt + (E < capacity_rows ? E : capacity_rows)) * ((F + nt - 1) / nt); };
+    // A pair where experts have rows for 256 (with 128 a half of its rows would be empty: 16 experts x 128 rows 65 us against 57) and there are
+    // tiles for more than a quarter of the GPU (2,048 rows of one expert, 1,024 features of 7,168: 19 against 17 us; 4,096 features: 35
+    // against 54).
+    const bool pairs = capacity_rows >= (int64_t)192 * E && capacity_rows / 256 * ((F + 255) / 256) * 15 >= 4 * sms;
+    const long long tiles = pairs ? 2 * most_tiles(256, 256) : most_tiles(128, 128);
+    const int grid = (int)(tiles < sms ? tiles : sms) / (pairs ? 2 : 1) * (pairs ? 2 : 1);
     CUtensorMap x_map, w_map;
     const cuuint64_t x_dims[2] = {(cuuint64_t)(K / 2), (cuuint64_t)capacity_rows}, x_strides[1] = {(cuuint64_t)x_codes_ld};
     const cuuint64_t w_dims[3] = {(cuuint64_t)(K / 2), (cuuint64_t)F, (cuuint64_t)E};
     const cuuint64_t w_strides[2] = {(cuuint64_t)(K / 2), (cuuint64_t)(K / 2) * (cuuint64_t)F};
-    if (!make_map(&x_map, 2, x_codes, x_dims, x_strides, kPrBox) || !make_map(&w_map, 3, w_codes, w_dims, w_strides, large ? 256 : 128))
+    if (!make_map(&x_map, 2, x_codes, x_dims, x_strides, kPrBox) || !make_map(&w_map, 3, w_codes, w_dims, w_strides, 128))
         return VP_E_CUDA;
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        const auto go = [&](auto fn, size_t smem) {
-            e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024);
-            if (e == cudaSuccess) e = launch_after(fn, grid, kPrThreads, smem, (cudaStream_t)cuda_stream, x_map, w_map, a);
-        };
-        if (large) go(mxfp4_product_kernel<256, X>, product_smem<256>(E));
-        else go(mxfp4_product_kernel<128, X>, product_smem<128>(E));
+        e = pairs ? launch_product<2, X>(x_map, w_map, a, grid, (cudaStream_t)cuda_stream)
+                  : launch_product<1, X>(x_map, w_map, a, grid, (cudaStream_t)cuda_stream);
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
 }
