@@ -15,7 +15,8 @@ namespace {
 
 constexpr int kCombineThreads = 256;
 constexpr int kSlots = 8;                         // slots whose rows are in flight together, at most
-constexpr int kGradThreads = 64, kGradStages = 5;  // (three to six stages, two or four warps: within 3 %)
+constexpr int kGradThreads = 64, kGradAhead = 5;   // (three to six stages, two or four warps: within 3 %)
+constexpr int kGradShared = 256;
 constexpr int kCombineMaxTop = 4096;              // (8 bytes of shared memory per slot)
 
 // A vector of a row that is there, zeros for one that is not (its memory may hold anything): loads under a predicate, no branch
@@ -110,20 +111,22 @@ __device__ __forceinline__ void copy_16(unsigned to, const void* from, bool here
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(here ? 16 : 0) : "memory");
 }
 
-// A warp per token and S slots.  Every lane copies the vectors that it will work on itself, kGradStages - 1 steps of 32 vectors ahead, so
+// A warp per token and S slots.  Every lane copies the vectors that it will work on itself, kGradAhead - 1 steps of 32 vectors ahead, so
 // that nothing waits for another thread and the loads in flight cost no registers: with loads into registers, one step at a time or two,
-// reads and writes together reached 4.9 to 6.1 TB/s (8,192 tokens x 8 of 4,096 bf16 186 to 235 us, 1,531 x 6 of 2,048 18 to 22); so 6.3 TB/s, 181 and
-// 17.4 us.
-template <typename T, int S>
-__global__ void __launch_bounds__(kGradThreads)
+// reads and writes together reached 4.9 to 6.1 TB/s (8,192 tokens x 8 of 4,096 bf16 186 to 235 us); so 168 us, 6.8 TB/s.
+// SHARED: the CTA's warps share a token and S slots (with few tokens a call would wait for one warp's steps one after another: a token of
+// 7,168 values, 28 steps, 16.7 us, so 4.6); their sums meet in a fixed order.
+template <typename T, int S, bool SHARED>
+__global__ void __launch_bounds__(SHARED ? kGradShared : kGradThreads)
 combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
-    constexpr int V = 16 / (int)sizeof(T);
+    constexpr int V = 16 / (int)sizeof(T), kGradStages = SHARED ? 2 : kGradAhead;
     extern __shared__ uint4 s_stage[];            // [warps][stages][S + 1][32]
+    __shared__ float s_part[SHARED ? kGradShared / 32 : 1][S];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_wait();
     const int batches = (a.topk + S - 1) / S;
-    const long long item = (long long)blockIdx.x * (kGradThreads / 32) + warp, t = item / batches;
-    if (t >= a.T) return;
+    const long long item = SHARED ? blockIdx.x : (long long)blockIdx.x * (kGradThreads / 32) + warp, t = item / batches;
+    if (!SHARED && t >= a.T) return;
     const int s0 = (int)(item % batches) * S, slots = min(S, a.topk - s0);
     const long long first = t * a.topk + s0, n = a.H / V;
     const int at = lane < slots ? a.idx[first + lane] : -1;
@@ -133,6 +136,7 @@ combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
     uint4* const grad_rows = (uint4*)a.grad_rows + first * n;
     uint4* const stage = s_stage + warp * kGradStages * (S + 1) * 32 + lane;
     const unsigned stage_at = (unsigned)__cvta_generic_to_shared(stage);
+    const int first_vector = SHARED ? (int)threadIdx.x : lane;
     const auto issue = [&](long long i, int k) {
         const unsigned to = stage_at + k * (S + 1) * 512;
         copy_16(to, grad + i, i < n);
@@ -146,10 +150,11 @@ combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
         w[s] = __shfl_sync(kAll, own, s);
         dot[s] = 0;
     }
+    constexpr int step = SHARED ? kGradShared : 32;
 #pragma unroll
-    for (int k = 0; k < kGradStages - 1; k++) issue(lane + 32 * k, k);
+    for (int k = 0; k < kGradStages - 1; k++) issue(first_vector + step * k, k);
     int k = 0;
-    for (long long i = lane; __any_sync(kAll, i < n); i += 32) {
+    for (long long i = first_vector; __any_sync(kAll, i < n); i += step) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kGradStages - 2) : "memory");
         const uint4* const from = stage + k * (S + 1) * 32;
         const Pack<T, V> g = *(const Pack<T, V>*)from;
@@ -163,7 +168,7 @@ combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
             for (int u = 0; u < V; u++) dot[s] = fmaf(f[u], value_of(x.v[u]), dot[s]);
         }
         const int last = k == 0 ? kGradStages - 1 : k - 1;
-        issue(i + 32 * (kGradStages - 1), last);
+        issue(i + step * (kGradStages - 1), last);
         if (a.grad_rows && i < n)
 #pragma unroll
             for (int s = 0; s < S; s++) {
@@ -182,6 +187,13 @@ combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
     for (int s = 0; s < S; s++) {
         const float d = warp_sum(dot[s]);
         if (lane == s) mine = d;
+    }
+    if (SHARED) {
+        if (lane < S) s_part[warp][lane] = mine;
+        __syncthreads();
+        mine = 0;
+        if (warp > 0) return;
+        for (int k = 0; k < kGradShared / 32 && lane < S; k++) mine += s_part[k][lane];
     }
     if (lane < slots) a.grad_weights[first + lane] = mine;
 }
@@ -270,6 +282,9 @@ extern "C" int vp_combine_backward(const void* grad, const void* rows, int dtype
     if ((uintptr_t)grad % size || (uintptr_t)rows % size || (uintptr_t)grad_rows % size) return VP_E_BAD_ARG;
     const CombineGradArgs a{grad, rows, expert_idx, weights, grad_rows, grad_weights, T, H, topk};
     const bool wide = vectors(size, H, {grad, rows, grad_rows});
+    const long long n = H * size / 16;
+    const int sms = sm_count_of_device();
+    if (!sms) return VP_E_CUDA;
     const auto ctas = [&](long long items) { return (int)((items + kGradThreads / 32 - 1) / (kGradThreads / 32)); };
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
@@ -280,10 +295,16 @@ extern "C" int vp_combine_backward(const void* grad, const void* rows, int dtype
         }
         with_slots(topk, [&](auto slots) {
             constexpr int s = decltype(slots)::value;
-            constexpr size_t smem = (size_t)(kGradThreads / 32) * kGradStages * (s + 1) * 512;
-            const auto fn = combine_backward_kernel<X, s>;
-            e = smem > 48 * 1024 ? cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
-            if (e == cudaSuccess) e = launch_after(fn, ctas((long long)T * ((topk + s - 1) / s)), kGradThreads, smem, (cudaStream_t)cuda_stream, a);
+            const long long items = (long long)T * ((topk + s - 1) / s);
+            const auto go = [&](auto fn, int grid, int threads, int stages) {
+                const size_t smem = (size_t)(threads / 32) * stages * (s + 1) * 512;
+                e = smem > 48 * 1024 ? cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+                if (e == cudaSuccess) e = launch_after(fn, grid, threads, smem, (cudaStream_t)cuda_stream, a);
+            };
+            // Warps share a token where rows are long or tokens few: 4,096 x 8 of 7,168 bf16 150 against 160 us, 128 x 8 of 1,024 2.5 against
+            // 4.0; 1,531 x 6 of 2,048 14.1 against 9.7.
+            if (n >= 512 || (items <= 4 * sms && n > 64)) go(combine_backward_kernel<X, s, true>, (int)items, kGradShared, 2);
+            else go(combine_backward_kernel<X, s, false>, ctas(items), kGradThreads, kGradAhead);
         });
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
