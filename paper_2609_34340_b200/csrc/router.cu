@@ -290,16 +290,18 @@ route_kernel(const __grid_constant__ RouteArgs a) {
                 mine = sum_of_two(hi, lo, a.group_top);
             }
         }
+        // topk_group times the best that is left, the lowest index among equals (groups without an expert that can be chosen need no choice).
         if (lane >= a.n_group) mine = -CUDART_INF_F;
-        int rank = 0;
-        for (int g = 0; g < a.n_group; g++) {
-            const float other = __shfl_sync(kAll, mine, g);
-            rank += other > mine || (other == mine && g < lane);
+        unsigned open = 0;
+        float worst_in = CUDART_INF_F;
+        for (int r = 0; r < a.topk_group; r++) {
+            worst_in = warp_max(mine);
+            const unsigned best = __ballot_sync(kAll, mine == worst_in);
+            open |= best & (0u - best);
+            if (open >> lane & 1) mine = -CUDART_INF_F;
         }
-        const bool in = lane < a.n_group && rank < a.topk_group;
-        unsigned open = __ballot_sync(kAll, in);
         if (rounded_groups) {                     // is the last group in clear of the first one out?
-            const float worst_in = warp_min(in ? mine : CUDART_INF_F), best_out = warp_max(in ? -CUDART_INF_F : mine);
+            const float best_out = warp_max(mine);
             if (best_out > -CUDART_INF_F && !(worst_in - best_out > 2 * tol)) {
                 float copy[VPL];                  // (z itself stays in registers)
 #pragma unroll
