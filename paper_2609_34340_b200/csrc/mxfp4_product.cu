@@ -181,32 +181,37 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a, const Experts& x, 
 }
 
 // 32 scales from byte k of a row of `bytes`; 1 behind its end and in rows that are not there.
-struct alignas(16) Scales { unsigned w[8]; };
+struct Scales { unsigned w[8]; };
+// The row's end, or a row at another alignment.  Out of line: inside the loop of every loader it cost instruction cache (decode 53 -> 68 us).
+__device__ __noinline__ Scales load_odd_scales(const uint8_t* p, int bytes) {
+    Scales v;
+#pragma unroll 1
+    for (int i = 0; i < 8; i++) {
+        unsigned w = 0x7f7f7f7f;
+        if (4 * i + 4 <= bytes && ((uintptr_t)p & 3) == 0) w = *(const unsigned*)(p + 4 * i);
+        else
+            for (int b = 0; b < 4; b++)
+                if (4 * i + b < bytes) w = (w & ~(255u << (8 * b))) | (unsigned)p[4 * i + b] << (8 * b);
+        v.w[i] = w;
+    }
+    return v;
+}
 __device__ __forceinline__ Scales load_scales(const uint8_t* row, int k, int bytes, bool there) {
     Scales v;
     const uint8_t* const p = row + k;
-    if (there && k + 32 <= bytes && ((uintptr_t)p & 31) == 0) {       // a sector at once: every part of it is a request to L2 of its own
+    const bool whole = k + 32 <= bytes;
+    if (there && whole && ((uintptr_t)p & 31) == 0) {                 // a sector at once: every part of it is a request to L2 of its own
         asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7]) : "l"(p));
-        return v;
+    } else if (there && whole && ((uintptr_t)p & 15) == 0) {
+        const uint4 a = *(const uint4*)p, b = *(const uint4*)(p + 16);
+        v = Scales{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+    } else if (there) {
+        v = load_odd_scales(p, min(bytes - k, 32));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v.w[i] = 0x7f7f7f7f;
     }
-#pragma unroll
-    for (int i = 0; i < 8; i++) v.w[i] = 0x7f7f7f7f;
-    if (!there) return v;
-#pragma unroll
-    for (int h = 0; h < 2; h++)
-        if (k + 16 * h + 16 <= bytes && ((uintptr_t)p & 15) == 0) {
-            *(uint4*)(v.w + 4 * h) = *(const uint4*)(p + 16 * h);
-        } else {
-#pragma unroll
-            for (int i = 4 * h; i < 4 * h + 4; i++) {
-                if (k + 4 * i + 4 <= bytes && ((uintptr_t)p & 3) == 0) v.w[i] = *(const unsigned*)(p + 4 * i);
-                else
-#pragma unroll
-                    for (int b = 0; b < 4; b++)
-                        if (k + 4 * i + b < bytes) v.w[i] = (v.w[i] & ~(255u << (8 * b))) | (unsigned)p[4 * i + b] << (8 * b);
-            }
-        }
     return v;
 }
 
