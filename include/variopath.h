@@ -540,7 +540,7 @@ int vp_route_backward(const vp_route_params* params, const void* logits, int dty
 /*
  * vp_combine - the weighted sum at the end of the layer: out[t] = base[t] + the sum over slots with expert_idx[t][s] >= 0 of
  * weights[t][s] * rows[t * topk + s], in 32 bits, slots in ascending order, rounded once.
- *   rows [T * topk][H], base [T][H] or NULL, out [T][H]: of `dtype`, contiguous; out may be base.  Rows of dropped copies
+ *   rows [T * topk][H], base [T][H] or NULL, out [T][H]: of `dtype`, contiguous; out may be base, not rows.  Rows of dropped copies
  *   (expert_idx < 0) are not read.  weights [T][topk] float.  topk <= 4096, else VP_E_UNSUPPORTED.
  */
 int vp_combine(const void* rows, int dtype, const int32_t* expert_idx, const float* weights, int T, int topk, int64_t H,
@@ -549,7 +549,7 @@ int vp_combine(const void* rows, int dtype, const int32_t* expert_idx, const flo
 /*
  * vp_combine_backward - grad_rows[t * topk + s] = weights[t][s] * grad[t] (0 for dropped copies: what vp_pack sends back) and
  * grad_weights[t][s] = <grad[t], rows[t * topk + s]> (0 for dropped copies).  Either output may be NULL, rows too when
- * grad_weights is.  The gradient of base is grad itself.
+ * grad_weights is.  No output may overlap an input.  The gradient of base is grad itself.
  */
 int vp_combine_backward(const void* grad, const void* rows, int dtype, const int32_t* expert_idx, const float* weights, int T,
                         int topk, int64_t H, void* grad_rows, float* grad_weights, void* cuda_stream);
@@ -570,7 +570,8 @@ int vp_combine_backward(const void* grad, const void* rows, int dtype, const int
  *   x       [rows][ld]: cols values per row (a multiple of 32); gated: 2 * cols, and the value quantised is
  *           silu(x[k]) * x[cols + k] in 32 bits (the activation between an expert's products)
  *   n_rows  int32[1] or NULL: rows in use (clamped to 0 .. rows); what lies behind them is neither read nor written
- *   codes   [rows][codes_ld], scales [rows][scales_ld] bytes
+ *   codes   [rows][codes_ld], scales [rows][scales_ld] bytes; rows and their parts may not overlap
+ * Rows, and bytes from a row to the next: below 2^31, else VP_E_UNSUPPORTED.
  */
 int vp_mxfp4_quantize(const void* x, int dtype, int64_t ld, int64_t rows, int64_t cols, int gated, const int32_t* n_rows,
                       uint8_t* codes, int64_t codes_ld, uint8_t* scales, int64_t scales_ld, void* cuda_stream);

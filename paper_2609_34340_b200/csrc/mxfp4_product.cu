@@ -12,6 +12,12 @@
 // operands, warps 2, 3 and 8 load scales and lay them out as the tensor core reads them, warp 1 (of the first CTA of a pair) issues the
 // copies of scales into tensor memory and the products, warps 4 to 7 bring finished tiles from tensor memory to the output while the next
 // tile is summed.
+//
+// What bounds it: with few rows per expert HBM, by which the matrices come (16 experts x 4,096 x 7,168, 128 rows: 49 us, 5.1 TB/s; without the loads of
+// scales 43, so a seventh is their latency); with many the operands' way from L2 to the SMs, 11 TB/s here (16,384 rows, 8 experts, 7,168 x 4,096: 175 us,
+// 5.5 PFLOP/s; the loads alone 176, the products alone 122); a single row is a chain of a third of a microsecond per 256 values of k
+// (7,168 x 4,096: 14.7 us).  Tried: scales through asynchronous copies to shared memory, or two to four chunks ahead in registers (1.1 to 1.5 times the
+// time), scales in tensor memory a stage ahead with barriers of their own (1.4 times), one CTA on 128 x 256 (274 us).
 #include <cuda.h>
 #include <type_traits>
 
@@ -24,7 +30,7 @@ constexpr int kPrMaxExperts = 1024;
 constexpr int kPrMaxK = 1 << 20, kPrMaxF = 1 << 20;      // (a matrix is below 2^40 bytes, a tile's sum below a millisecond)
 constexpr int kPrM = 128;                         // rows of a tile: lanes of tensor memory
 constexpr int kPrK = 256;                         // values of k per stage: one swizzle atom of 128 bytes
-constexpr int kPrBox = 32;                        // rows per TMA box of the rows' operand
+constexpr int kPrBox = 32;                        // rows of a TMA box that is not a whole operand's (which cost as much as their bytes: 212 -> 175 us with one of 128)
 constexpr int kPrThreads = 320;
 constexpr int kPrLine = 64;                       // bytes of an output row that leave together
 constexpr unsigned kPrPolls = 1u << 22;
@@ -297,7 +303,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
             s_n = n;
             s_most = most;
             // One CTA: tiles of 128, 96, 64 or 32 features, by the turns of the CTAs and the rows of operands that a turn fetches (or the time that
-            // it takes to issue its products, about that of 90 rows).  One row of one expert, 4,096 features of 7,168: NT_FIGURE.
+            // it takes to issue its products, about that of 90 rows).  8 experts of one row each, 4,096 features of 7,168: 29.2 us with 128, so 27.3.
             int best = S::NT, least = 0x7fffffff;
             for (int nt = 128; CG == 1 && nt >= 32; nt -= 32) {
                 const long long all = (long long)tiles * ((a.F + nt - 1) / nt), turns = (all + gridDim.x - 1) / gridDim.x;
@@ -459,8 +465,8 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
             }
         }
     } else if (warp == 9) {
-        // Makes scales that are written visible to the tensor core's copies.  The fence is a warp's own that has no loads on their way: in the
-        // warps that load scales it waits for those.
+        // Makes scales that are written visible to the tensor core's copies: by a warp that has no loads on their way, for which the fence would
+        // wait in the warps that load.  (What it fences has been seen by its wait; the arrival behind it is what the copies wait for.)
         if (lane == 0) {
             bool ok = true;
             for (long long t = t0; ok && t < tiles; t += step)
@@ -591,7 +597,8 @@ template <int CG>
 size_t product_smem(int E) { return (size_t)Shape<CG>::lists_begin + 1024 + (size_t)E * 6 + 4; }
 
 template <int CG, typename T>
-cudaError_t launch_product(const CUtensorMap& x_map, const CUtensorMap& w_map, const CUtensorMap& w_part_map, const ProductArgs& a, int grid, cudaStream_t stream) {
+cudaError_t launch_product(const CUtensorMap& x_map, const CUtensorMap& w_map, const CUtensorMap& w_part_map, const ProductArgs& a, int grid,
+                           cudaStream_t stream) {
     const auto fn = mxfp4_product_kernel<CG, T>;
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)product_smem<CG>(kPrMaxExperts));
     if (e != cudaSuccess) return e;
@@ -632,9 +639,9 @@ extern "C" int vp_mxfp4_product(const uint8_t* x_codes, int64_t x_codes_ld, cons
                         (uintptr_t)out % 16 == 0 && out_ld * size % 16 == 0, status};
     // Row tiles there can be at most: a part of one per expert more than the rows fill.
     const auto most_tiles = [&](int mt, int nt) { return ((capacity_rows + mt - 1) / mt + (E < capacity_rows ? E : capacity_rows)) * ((F + nt - 1) / nt); };
-    // A pair where experts have rows for 256 (with 128 a half of its rows would be empty: 16 experts x 128 rows 65 us against 57) and there are
-    // tiles for more than a quarter of the GPU (2,048 rows of one expert, 1,024 features of 7,168: 19 against 17 us; 4,096 features: 35
-    // against 54).
+    // A pair where experts have rows for 256 (16 x 128 rows, half of a pair's rows empty: 65 us against 57 of one CTA; 8 x 384 63 against 80) and
+    // there are tiles for more than a quarter of the GPU (2,048 rows of one expert, 1,024 features of 7,168: 19 against 17 us; 4,096
+    // features: 35 against 54).
     const bool pairs = capacity_rows >= (int64_t)192 * E && capacity_rows / 256 * ((F + 255) / 256) * 15 >= 4 * sms;
     const long long tiles = pairs ? 2 * most_tiles(256, 256) : most_tiles(128, kPrBox);
     const int grid = (int)(tiles < sms ? tiles : sms) / (pairs ? 2 : 1) * (pairs ? 2 : 1);
