@@ -245,7 +245,7 @@ extern "C" int vp_combine(const void* rows, int dtype, const int32_t* expert_idx
     if (T == 0) return VP_OK;
     if (!rows || !expert_idx || !weights || !out) return VP_E_BAD_ARG;
     const int size = size_of_type(dtype);
-    if ((uintptr_t)rows % size || (uintptr_t)base % size || (uintptr_t)out % size) return VP_E_BAD_ARG;
+    if ((uintptr_t)rows % size || (uintptr_t)base % size || (uintptr_t)out % size || ((uintptr_t)expert_idx | (uintptr_t)weights) % 4) return VP_E_BAD_ARG;
     const int sms = sm_count_of_device();
     if (!sms) return VP_E_CUDA;
     CombineArgs a{rows, base, expert_idx, weights, out, T, H, topk, 1, 1};
@@ -279,7 +279,9 @@ extern "C" int vp_combine_backward(const void* grad, const void* rows, int dtype
     if (T == 0) return VP_OK;
     if (!grad || !expert_idx || !weights || (!grad_rows && !grad_weights) || (grad_weights && !rows)) return VP_E_BAD_ARG;
     const int size = size_of_type(dtype);
-    if ((uintptr_t)grad % size || (uintptr_t)rows % size || (uintptr_t)grad_rows % size) return VP_E_BAD_ARG;
+    if ((uintptr_t)grad % size || (uintptr_t)rows % size || (uintptr_t)grad_rows % size ||
+        ((uintptr_t)expert_idx | (uintptr_t)weights | (uintptr_t)grad_weights) % 4)
+        return VP_E_BAD_ARG;
     const CombineGradArgs a{grad, rows, expert_idx, weights, grad_rows, grad_weights, T, H, topk};
     const bool wide = vectors(size, H, {grad, rows, grad_rows});
     const long long n = H * size / 16;

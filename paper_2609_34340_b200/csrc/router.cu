@@ -554,7 +554,7 @@ extern "C" int vp_route(const vp_route_params* p, const void* logits, int dtype,
     if (T == 0) return VP_OK;
     if (!logits || !expert_idx || !weights) return VP_E_BAD_ARG;
     const int size = size_of_type(dtype);
-    if ((uintptr_t)logits % size) return VP_E_BAD_ARG;
+    if ((uintptr_t)logits % size || ((uintptr_t)expert_idx | (uintptr_t)weights | (uintptr_t)bias) % 4) return VP_E_BAD_ARG;
     const int sms = sm_count_of_device();
     if (!sms) return VP_E_CUDA;
     RouteArgs a;
@@ -587,7 +587,7 @@ extern "C" int vp_route_backward(const vp_route_params* p, const void* logits, i
     if (T == 0) return VP_OK;
     if (!logits || !expert_idx || !grad_weights || !grad_logits) return VP_E_BAD_ARG;
     const int size = size_of_type(dtype);
-    if ((uintptr_t)logits % size || (uintptr_t)grad_logits % size) return VP_E_BAD_ARG;
+    if ((uintptr_t)logits % size || (uintptr_t)grad_logits % size || ((uintptr_t)expert_idx | (uintptr_t)grad_weights) % 4) return VP_E_BAD_ARG;
     const int sms = sm_count_of_device();
     if (!sms) return VP_E_CUDA;
     RouteGradArgs a;

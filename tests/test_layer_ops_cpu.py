@@ -44,6 +44,8 @@ def test_route_refusals(lib):
         assert fn(_params(), logits=null) == -1 and fn(_params(), idx=null) == -1 and fn(_params(), logits=P((1 << 20) + 2)) == -1
         assert fn(_params(topk=32, topk_group=8), T=1 << 26) == -6
         assert fn(_params(), T=0, logits=null) == 0
+    odd = P((1 << 20) + 2)
+    assert route(_params(), idx=odd) == -1 and route(_params(), w=odd) == -1 and backward(_params(), idx=odd) == -1 and backward(_params(), g=odd) == -1
     assert route(_params(), w=null) == -1 and backward(_params(), g=null) == -1 and backward(_params(), out=null) == -1
     assert backward(_params(), out_ld=63) == -1
 
@@ -61,6 +63,9 @@ def test_combine_refusals(lib):
             assert fn(**bad) == -1, bad
         assert fn(T=1 << 30, topk=4) == -6
         assert fn(T=0, rows=null, idx=null) == 0
+    odd = P((1 << 20) + 2)
+    assert combine(idx=odd) == -1 and combine(w=odd) == -1 and backward(idx=odd) == -1 and backward(w=odd) == -1 and backward(gw=odd) == -1
+    assert combine(topk=5000, T=1) == -6
     assert combine(out=null) == -1 and combine(base=P((1 << 20) + 1)) == -1
     assert backward(grad=null) == -1 and backward(gr=null, gw=null) == -1
 
