@@ -13,10 +13,10 @@
 // copies of scales into tensor memory and the products, warps 4 to 7 bring finished tiles from tensor memory to the output while the next
 // tile is summed.
 //
-// What bounds it: with few rows per expert HBM, by which the matrices come (16 experts x 4,096 x 7,168, 128 rows: 49 us, 5.1 TB/s; without the loads of
+// What bounds it: with few rows per expert HBM, by which the matrices come (16 experts x 4,096 x 7,168, 128 rows: 48 us, 5.2 TB/s; without the loads of
 // scales 43, so a seventh is their latency); with many the operands' way from L2 to the SMs, 11 TB/s here (16,384 rows, 8 experts, 7,168 x 4,096: 175 us,
 // 5.5 PFLOP/s; the loads alone 176, the products alone 122); a single row is a chain of a third of a microsecond per 256 values of k
-// (7,168 x 4,096: 14.7 us).  Tried: scales through asynchronous copies to shared memory, or two to four chunks ahead in registers (1.1 to 1.5 times the
+// (7,168 x 4,096: 12.7 us).  Tried: scales through asynchronous copies to shared memory, or two to four chunks ahead in registers (1.1 to 1.5 times the
 // time), scales in tensor memory a stage ahead with barriers of their own (1.4 times), one CTA on 128 x 256 (274 us).
 #include <cuda.h>
 #include <type_traits>
@@ -30,7 +30,7 @@ constexpr int kPrMaxExperts = 1024;
 constexpr int kPrMaxK = 1 << 20, kPrMaxF = 1 << 20;      // (a matrix is below 2^40 bytes, a tile's sum below a millisecond)
 constexpr int kPrM = 128;                         // rows of a tile: lanes of tensor memory
 constexpr int kPrK = 256;                         // values of k per stage: one swizzle atom of 128 bytes
-constexpr int kPrBox = 32;                        // rows of a TMA box that is not a whole operand's (which cost as much as their bytes: 212 -> 175 us with one of 128)
+constexpr int kPrBox = 32;                        // rows of a TMA box that is not a whole operand's
 constexpr int kPrThreads = 320;
 constexpr int kPrLine = 64;                       // bytes of an output row that leave together
 constexpr unsigned kPrPolls = 1u << 22;
@@ -38,8 +38,8 @@ constexpr unsigned kPrPolls = 1u << 22;
 // CG: CTAs that share a tile.
 template <int CG>
 struct Shape {
-    static constexpr int NT = 128 * CG;           // features of a tile, at most
-    static constexpr int a_bytes = kPrM * (kPrK / 2), b_bytes = 128 * (kPrK / 2);           // operands of a stage, per CTA, at most
+    static constexpr int NT = 128 * CG;           // features of a tile
+    static constexpr int a_bytes = kPrM * (kPrK / 2), b_bytes = 128 * (kPrK / 2);           // operands of a stage, per CTA (of rows at most)
     static constexpr int sa_bytes = kPrM * (kPrK / 32), s_bytes = sa_bytes + NT * (kPrK / 32);        // scales (every CTA holds all features')
     static constexpr int stages = CG == 1 ? 6 : 5, most_stages = CG == 1 ? 16 : 5;
     static constexpr int out_begin = stages * (a_bytes + b_bytes + s_bytes);
@@ -223,14 +223,14 @@ __device__ __forceinline__ Scales load_scales(const uint8_t* row, int k, int byt
 
 template <int CG, typename T>
 __global__ void __launch_bounds__(kPrThreads, 1)
-mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map,
-                     const __grid_constant__ CUtensorMap w_part_map, const __grid_constant__ ProductArgs a) {
+mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap x_part_map,
+                     const __grid_constant__ CUtensorMap w_map, const __grid_constant__ ProductArgs a) {
     using S = Shape<CG>;
-    constexpr int MT = kPrM * CG;
+    constexpr int NT = S::NT, MT = kPrM * CG;
     extern __shared__ unsigned char s_raw[];
     __shared__ uint64_t s_bar[3 * S::most_stages + 5];
     __shared__ unsigned s_tmem;
-    __shared__ int s_n, s_most, s_nt;
+    __shared__ int s_n, s_most;
     __shared__ volatile int s_stop;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x % CG);          // of the pair
@@ -302,15 +302,6 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
             ex.tiles[n] = tiles;
             s_n = n;
             s_most = most;
-            // One CTA: tiles of 128, 96, 64 or 32 features, by the turns of the CTAs and the rows of operands that a turn fetches (or the time that
-            // it takes to issue its products, about that of 90 rows).  8 experts of one row each, 4,096 features of 7,168: 29.2 us with 128, so 27.3.
-            int best = S::NT, least = 0x7fffffff;
-            for (int nt = 128; CG == 1 && nt >= 32; nt -= 32) {
-                const long long all = (long long)tiles * ((a.F + nt - 1) / nt), turns = (all + gridDim.x - 1) / gridDim.x;
-                const long long cost = turns * max(nt + min((most + kPrBox - 1) / kPrBox * kPrBox, kPrM), 90);
-                if (cost < least) { least = (int)cost; best = nt; }
-            }
-            s_nt = best;
         }
         if (bad && blockIdx.x == 0) atomicOr(a.status, VP_ST_PACK_MISMATCH);
     }
@@ -320,7 +311,6 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     fence_after();
     ex.n = s_n;
     const unsigned tmem = s_tmem;
-    const int NT = CG == 1 ? s_nt : S::NT;
     const int n_tiles = (a.F + NT - 1) / NT, k_tiles = (a.K + kPrK - 1) / kPrK;
     const long long tiles = (long long)ex.tiles[ex.n] * n_tiles, t0 = blockIdx.x / CG, step = gridDim.x / CG;
     // Every wait is bounded: the one that gives up sets the flag, which ends the others' (of the other CTA by their own limits).
@@ -334,37 +324,35 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
         return false;
     };
     // One CTA: where no expert has more than 32, 64 or 96 rows, a stage holds that many, and there are more stages (the products read 128
-    // rows all the same: what lies behind, any bits being numbers, makes rows that nobody stores).
+    // rows all the same: what lies behind, any bits being numbers, makes rows that nobody stores).  Otherwise all rows come as one box,
+    // whosever they are: four boxes of 32 cost as much time as their bytes (16,384 rows, 7,168 x 4,096: 212 us against 175), which is also
+    // why tiles do not get narrower where CTAs are idle (one row of one expert 14.7 us with 32 features a tile, 12.7 with 128).
     const int a_bytes = CG == 1 ? min((s_most + kPrBox - 1) / kPrBox * kPrBox * (kPrK / 2), S::a_bytes) : S::a_bytes;
-    const int b_bytes = CG == 1 ? NT * (kPrK / 2) : S::b_bytes;
-    const int stages = CG == 1 ? min(S::out_begin / (a_bytes + b_bytes + S::s_bytes), S::most_stages) : S::stages;
+    const int stages = CG == 1 ? min(S::out_begin / (a_bytes + S::b_bytes + S::s_bytes), S::most_stages) : S::stages;
     struct Ring {                                 // a place of a ring of barriers, and the parity of its turn
         int at;
         unsigned phase;
         __device__ __forceinline__ void next(int n) { if (++at == n) { at = 0; phase ^= 1; } }
     };
     Ring s{0, 0};
-    const auto stage_at = [&](int st) { return base + st * (a_bytes + b_bytes + S::s_bytes); };
-    const auto scales_at = [&](int st) { return stage_at(st) + a_bytes + b_bytes; };
+    const auto stage_at = [&](int st) { return base + st * (a_bytes + S::b_bytes + S::s_bytes); };
+    const auto scales_at = [&](int st) { return stage_at(st) + a_bytes + S::b_bytes; };
 
     if (warp == 0) {
         if (lane == 0) {
             bool ok = true;
             for (long long t = t0; ok && t < tiles; t += step) {
                 const Tile tile = tile_of(a, ex, t, n_tiles, MT, NT);
-                // A pair loads all its 128 rows with one instruction, whosever they are; one CTA those it needs, 32 at a time.
-                const int rows = min(tile.rows, kPrM), box = CG > 1 ? kPrM : kPrBox, boxes = CG > 1 ? 1 : (rows + kPrBox - 1) / kPrBox;
+                const bool whole = CG > 1 || a_bytes == S::a_bytes;
+                const int boxes = whole ? 1 : (tile.rows + kPrBox - 1) / kPrBox, bytes = (whole ? kPrM : boxes * kPrBox) * (kPrK / 2) + S::b_bytes;
                 for (int k = 0; k < k_tiles; k++) {
                     if (!(ok = wait(empty(s.at), s.phase ^ 1))) break;
-                    const unsigned at = stage_at(s.at), bar = first_cta(full(s.at)), bytes = boxes * box * (kPrK / 2) + b_bytes;
+                    const unsigned at = stage_at(s.at), bar = first_cta(full(s.at));
                     if (CG == 1) mbar_expect_tx(bar, bytes);
                     else cluster_expect_tx(bar, bytes);
-                    if (CG > 1 || NT == 128) tma_3d<CG>(at + a_bytes, &w_map, k * (kPrK / 2), tile.n0 + rank * 128, tile.e, bar);
-                    else
-                        for (int b = 0; b < NT; b += kPrBox)
-                            tma_3d<CG>(at + a_bytes + b * (kPrK / 2), &w_part_map, k * (kPrK / 2), tile.n0 + b, tile.e, bar);
+                    tma_3d<CG>(at + a_bytes, &w_map, k * (kPrK / 2), tile.n0 + rank * 128, tile.e, bar);
                     for (int b = 0; b < boxes; b++)
-                        tma_2d<CG>(at + b * kPrBox * (kPrK / 2), &x_map, k * (kPrK / 2), tile.first + rank * kPrM + b * box, bar);
+                        tma_2d<CG>(at + b * kPrBox * (kPrK / 2), whole ? &x_map : &x_part_map, k * (kPrK / 2), tile.first + rank * kPrM + b * kPrBox, bar);
                     s.next(stages);
                 }
             }
@@ -381,9 +369,8 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
         if (rank == 0) {
             const unsigned tm = __reduce_max_sync(kAll, tmem), rows_bytes = __reduce_max_sync(kAll, (unsigned)a_bytes),
                            b16 = __reduce_max_sync(kAll, base) >> 4, n_stages = __reduce_max_sync(kAll, (unsigned)stages),
-                           nt = __reduce_max_sync(kAll, (unsigned)NT), feature_bytes = CG == 1 ? nt * (kPrK / 2) : S::b_bytes,
-                           stage16 = (rows_bytes + feature_bytes + S::s_bytes) >> 4,
-                           idesc = 1u << 7 | 1u << 10 | (nt >> 3) << 17 | 1u << 23 | (unsigned)(MT >> 7) << 27;
+                           stage16 = (rows_bytes + S::b_bytes + S::s_bytes) >> 4;
+            constexpr unsigned idesc = 1u << 7 | 1u << 10 | (unsigned)(NT >> 3) << 17 | 1u << 23 | (unsigned)(MT >> 7) << 27;
             const int my_tiles = __reduce_max_sync(kAll, t0 < tiles ? (int)((tiles - 1 - t0) / step) + 1 : 0);
             const bool one = elect_one();
             bool ok = true;
@@ -395,18 +382,18 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
                 for (int k = 0; k < k_tiles; k++) {
                     if (!(ok = __all_sync(kAll, wait(full(st), parity)))) break;
                     fence_after();
-                    const unsigned at16 = b16 + st * stage16, sa16 = at16 + ((rows_bytes + feature_bytes) >> 4);
+                    const unsigned at16 = b16 + st * stage16, sa16 = at16 + ((rows_bytes + S::b_bytes) >> 4);
                     const unsigned ta = tm + S::scales_at + st * S::scale_cols, tb = ta + 8;
                     if (one) {
 #pragma unroll
                         for (int c = 0; c < 2; c++) copy_scales<CG>(ta + 4 * c, desc_of(kScaleDesc, sa16 + 32 * c));
 #pragma unroll
-                        for (int c = 0; c < S::NT / 64; c++) copy_scales<CG>(tb + 4 * c, desc_of(kScaleDesc, sa16 + S::sa_bytes / 16 + 32 * c));
+                        for (int c = 0; c < NT / 64; c++) copy_scales<CG>(tb + 4 * c, desc_of(kScaleDesc, sa16 + S::sa_bytes / 16 + 32 * c));
 #pragma unroll
                         for (int u = 0; u < 4; u++) {         // 64 values of k each; two of a word's four scales
                             const unsigned half = (u & 1) * 2;
                             mma_mxf4<CG>(d, desc_of(kOperandDesc, at16 + 2 * u), desc_of(kOperandDesc, at16 + (rows_bytes >> 4) + 2 * u),
-                                         idesc | half << 29 | half << 4, ta + 4 * (u / 2), tb + S::NT / 32 * (u / 2), k > 0 || u > 0);
+                                         idesc | half << 29 | half << 4, ta + 4 * (u / 2), tb + NT / 32 * (u / 2), k > 0 || u > 0);
                         }
                         mma_commit<CG>(empty(st));
                     }
@@ -434,7 +421,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 const int r = lane + 32 * j + (is_b ? 128 * half : kPrM * rank);
-                const bool there = is_b ? r < NT && tile.n0 + r < a.F : r < tile.rows;
+                const bool there = is_b ? tile.n0 + r < a.F : r < tile.rows;
                 const uint8_t* const row = is_b ? a.ws + ((long long)tile.e * a.F + tile.n0 + r) * bytes
                                                 : a.xs + (long long)(tile.first + r) * a.xs_ld;
                 v[j] = load_scales(row, chunk * 32, bytes, there);
@@ -542,7 +529,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
             if (rows > 0)
 #pragma unroll
                 for (int c = 0; c < 4 * per; c++)
-                    if ((c0 * per + c) * cols < NT && tile.n0 + (c0 * per + c) * cols < a.F) store(&v[c / per], c0 * per + c);
+                    if (tile.n0 + (c0 * per + c) * cols < a.F) store(&v[c / per], c0 * per + c);
             if (CG > 1) {
                 const int c1 = c0 ^ 4;
 #pragma unroll
@@ -597,7 +584,7 @@ template <int CG>
 size_t product_smem(int E) { return (size_t)Shape<CG>::lists_begin + 1024 + (size_t)E * 6 + 4; }
 
 template <int CG, typename T>
-cudaError_t launch_product(const CUtensorMap& x_map, const CUtensorMap& w_map, const CUtensorMap& w_part_map, const ProductArgs& a, int grid,
+cudaError_t launch_product(const CUtensorMap& x_map, const CUtensorMap& x_part_map, const CUtensorMap& w_map, const ProductArgs& a, int grid,
                            cudaStream_t stream) {
     const auto fn = mxfp4_product_kernel<CG, T>;
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)product_smem<CG>(kPrMaxExperts));
@@ -615,7 +602,7 @@ cudaError_t launch_product(const CUtensorMap& x_map, const CUtensorMap& w_map, c
     cfg.attrs = at;
     cfg.numAttrs = CG > 1 ? 2 : 1;
     g_vp_launches++;
-    return cudaLaunchKernelEx(&cfg, fn, x_map, w_map, w_part_map, a);
+    return cudaLaunchKernelEx(&cfg, fn, x_map, x_part_map, w_map, a);
 }
 
 }  // namespace
@@ -643,20 +630,20 @@ extern "C" int vp_mxfp4_product(const uint8_t* x_codes, int64_t x_codes_ld, cons
     // there are tiles for more than a quarter of the GPU (2,048 rows of one expert, 1,024 features of 7,168: 19 against 17 us; 4,096
     // features: 35 against 54).
     const bool pairs = capacity_rows >= (int64_t)192 * E && capacity_rows / 256 * ((F + 255) / 256) * 15 >= 4 * sms;
-    const long long tiles = pairs ? 2 * most_tiles(256, 256) : most_tiles(128, kPrBox);
+    const long long tiles = pairs ? 2 * most_tiles(256, 256) : most_tiles(128, 128);
     const int grid = (int)(tiles < sms ? tiles : sms) / (pairs ? 2 : 1) * (pairs ? 2 : 1);
-    CUtensorMap x_map, w_map, w_part_map;
+    CUtensorMap x_map, x_part_map, w_map;
     const cuuint64_t x_dims[2] = {(cuuint64_t)(K / 2), (cuuint64_t)capacity_rows}, x_strides[1] = {(cuuint64_t)x_codes_ld};
     const cuuint64_t w_dims[3] = {(cuuint64_t)(K / 2), (cuuint64_t)F, (cuuint64_t)E};
     const cuuint64_t w_strides[2] = {(cuuint64_t)(K / 2), (cuuint64_t)(K / 2) * (cuuint64_t)F};
-    if (!make_map(&x_map, 2, x_codes, x_dims, x_strides, pairs ? kPrM : kPrBox) || !make_map(&w_map, 3, w_codes, w_dims, w_strides, 128) ||
-        !make_map(&w_part_map, 3, w_codes, w_dims, w_strides, kPrBox))
+    if (!make_map(&x_map, 2, x_codes, x_dims, x_strides, kPrM) || !make_map(&x_part_map, 2, x_codes, x_dims, x_strides, kPrBox) ||
+        !make_map(&w_map, 3, w_codes, w_dims, w_strides, 128))
         return VP_E_CUDA;
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        e = pairs ? launch_product<2, X>(x_map, w_map, w_part_map, a, grid, (cudaStream_t)cuda_stream)
-                  : launch_product<1, X>(x_map, w_map, w_part_map, a, grid, (cudaStream_t)cuda_stream);
+        e = pairs ? launch_product<2, X>(x_map, x_part_map, w_map, a, grid, (cudaStream_t)cuda_stream)
+                  : launch_product<1, X>(x_map, x_part_map, w_map, a, grid, (cudaStream_t)cuda_stream);
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
 }
