@@ -30,7 +30,7 @@ constexpr int kPrMaxExperts = 1024;
 constexpr int kPrMaxK = 1 << 20, kPrMaxF = 1 << 20;      // (a matrix is below 2^40 bytes, a tile's sum below a millisecond)
 constexpr int kPrM = 128;                         // rows of a tile: lanes of tensor memory
 constexpr int kPrK = 256;                         // values of k per stage: one swizzle atom of 128 bytes
-constexpr int kPrBox = 32;                        // rows of a TMA box that is not a whole operand's
+constexpr int kPrBox = 32;                        // the least rows of a stage
 constexpr int kPrThreads = 320;
 constexpr int kPrLine = 64;                       // bytes of an output row that leave together
 constexpr unsigned kPrPolls = 1u << 22;
@@ -223,8 +223,8 @@ __device__ __forceinline__ Scales load_scales(const uint8_t* row, int k, int byt
 
 template <int CG, typename T>
 __global__ void __launch_bounds__(kPrThreads, 1)
-mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap x_part_map,
-                     const __grid_constant__ CUtensorMap w_map, const __grid_constant__ ProductArgs a) {
+mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap x_64_map,
+                     const __grid_constant__ CUtensorMap x_32_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ ProductArgs a) {
     using S = Shape<CG>;
     constexpr int NT = S::NT, MT = kPrM * CG;
     extern __shared__ unsigned char s_raw[];
@@ -323,11 +323,11 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
         atomicOr(a.status, VP_ST_INTERNAL_TIMEOUT);
         return false;
     };
-    // One CTA: where no expert has more than 32, 64 or 96 rows, a stage holds that many, and there are more stages (the products read 128
-    // rows all the same: what lies behind, any bits being numbers, makes rows that nobody stores).  Otherwise all rows come as one box,
-    // whosever they are: four boxes of 32 cost as much time as their bytes (16,384 rows, 7,168 x 4,096: 212 us against 175), which is also
-    // why tiles do not get narrower where CTAs are idle (one row of one expert 14.7 us with 32 features a tile, 12.7 with 128).
-    const int a_bytes = CG == 1 ? min((s_most + kPrBox - 1) / kPrBox * kPrBox * (kPrK / 2), S::a_bytes) : S::a_bytes;
+    // One CTA: where no expert has more than 32 or 64 rows, a stage holds that many, and there are more stages (the products read 128 rows
+    // all the same: what lies behind, any bits being numbers, makes rows that nobody stores).  They come as one box, whosever they are:
+    // four boxes of 32 cost as much time as their bytes (16,384 rows, 7,168 x 4,096: 212 us against 175), which is also why tiles do not
+    // get narrower where CTAs are idle (one row of one expert 14.7 us with 32 features a tile, 12.7 with 128).
+    const int a_rows = CG > 1 || s_most > 2 * kPrBox ? kPrM : (s_most > kPrBox ? 2 * kPrBox : kPrBox), a_bytes = a_rows * (kPrK / 2);
     const int stages = CG == 1 ? min(S::out_begin / (a_bytes + S::b_bytes + S::s_bytes), S::most_stages) : S::stages;
     struct Ring {                                 // a place of a ring of barriers, and the parity of its turn
         int at;
@@ -343,16 +343,15 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
             bool ok = true;
             for (long long t = t0; ok && t < tiles; t += step) {
                 const Tile tile = tile_of(a, ex, t, n_tiles, MT, NT);
-                const bool whole = CG > 1 || a_bytes == S::a_bytes;
-                const int boxes = whole ? 1 : (tile.rows + kPrBox - 1) / kPrBox, bytes = (whole ? kPrM : boxes * kPrBox) * (kPrK / 2) + S::b_bytes;
+                const CUtensorMap* const map = a_rows == kPrM ? &x_map : (a_rows == kPrBox ? &x_32_map : &x_64_map);
+                const int bytes = a_bytes + S::b_bytes;
                 for (int k = 0; k < k_tiles; k++) {
                     if (!(ok = wait(empty(s.at), s.phase ^ 1))) break;
                     const unsigned at = stage_at(s.at), bar = first_cta(full(s.at));
                     if (CG == 1) mbar_expect_tx(bar, bytes);
                     else cluster_expect_tx(bar, bytes);
                     tma_3d<CG>(at + a_bytes, &w_map, k * (kPrK / 2), tile.n0 + rank * 128, tile.e, bar);
-                    for (int b = 0; b < boxes; b++)
-                        tma_2d<CG>(at + b * kPrBox * (kPrK / 2), whole ? &x_map : &x_part_map, k * (kPrK / 2), tile.first + rank * kPrM + b * kPrBox, bar);
+                    tma_2d<CG>(at, map, k * (kPrK / 2), tile.first + rank * kPrM, bar);
                     s.next(stages);
                 }
             }
@@ -584,7 +583,7 @@ template <int CG>
 size_t product_smem(int E) { return (size_t)Shape<CG>::lists_begin + 1024 + (size_t)E * 6 + 4; }
 
 template <int CG, typename T>
-cudaError_t launch_product(const CUtensorMap& x_map, const CUtensorMap& x_part_map, const CUtensorMap& w_map, const ProductArgs& a, int grid,
+cudaError_t launch_product(const CUtensorMap (&x_maps)[3], const CUtensorMap& w_map, const ProductArgs& a, int grid,
                            cudaStream_t stream) {
     const auto fn = mxfp4_product_kernel<CG, T>;
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)product_smem<CG>(kPrMaxExperts));
@@ -602,7 +601,7 @@ cudaError_t launch_product(const CUtensorMap& x_map, const CUtensorMap& x_part_m
     cfg.attrs = at;
     cfg.numAttrs = CG > 1 ? 2 : 1;
     g_vp_launches++;
-    return cudaLaunchKernelEx(&cfg, fn, x_map, x_part_map, w_map, a);
+    return cudaLaunchKernelEx(&cfg, fn, x_maps[0], x_maps[1], x_maps[2], w_map, a);
 }
 
 }  // namespace
@@ -632,18 +631,18 @@ extern "C" int vp_mxfp4_product(const uint8_t* x_codes, int64_t x_codes_ld, cons
     const bool pairs = capacity_rows >= (int64_t)192 * E && capacity_rows / 256 * ((F + 255) / 256) * 15 >= 4 * sms;
     const long long tiles = pairs ? 2 * most_tiles(256, 256) : most_tiles(128, 128);
     const int grid = (int)(tiles < sms ? tiles : sms) / (pairs ? 2 : 1) * (pairs ? 2 : 1);
-    CUtensorMap x_map, x_part_map, w_map;
+    CUtensorMap x_maps[3], w_map;             // of 128, 64 and 32 rows
     const cuuint64_t x_dims[2] = {(cuuint64_t)(K / 2), (cuuint64_t)capacity_rows}, x_strides[1] = {(cuuint64_t)x_codes_ld};
     const cuuint64_t w_dims[3] = {(cuuint64_t)(K / 2), (cuuint64_t)F, (cuuint64_t)E};
     const cuuint64_t w_strides[2] = {(cuuint64_t)(K / 2), (cuuint64_t)(K / 2) * (cuuint64_t)F};
-    if (!make_map(&x_map, 2, x_codes, x_dims, x_strides, kPrM) || !make_map(&x_part_map, 2, x_codes, x_dims, x_strides, kPrBox) ||
-        !make_map(&w_map, 3, w_codes, w_dims, w_strides, 128))
-        return VP_E_CUDA;
+    if (!make_map(&w_map, 3, w_codes, w_dims, w_strides, 128)) return VP_E_CUDA;
+    for (int i = 0; i < 3; i++)
+        if (!make_map(&x_maps[i], 2, x_codes, x_dims, x_strides, i == 0 ? kPrM : 2 * kPrBox / i)) return VP_E_CUDA;
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
-        e = pairs ? launch_product<2, X>(x_map, x_part_map, w_map, a, grid, (cudaStream_t)cuda_stream)
-                  : launch_product<1, X>(x_map, x_part_map, w_map, a, grid, (cudaStream_t)cuda_stream);
+        e = pairs ? launch_product<2, X>(x_maps, w_map, a, grid, (cudaStream_t)cuda_stream)
+                  : launch_product<1, X>(x_maps, w_map, a, grid, (cudaStream_t)cuda_stream);
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
 }
