@@ -186,39 +186,59 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a, const Experts& x, 
     return Tile{x.id[lo], r.first + m * mt, min(mt, r.n - m * mt), q / m_tiles * nt};
 }
 
-// 32 scales from byte k of a row of `bytes`; 1 behind its end and in rows that are not there.
+// 32 scales of a row.
 struct Scales { unsigned w[8]; };
-// The row's end, or a row at another alignment.  Out of line: inside the loop of every loader it cost instruction cache (decode 53 -> 68 us).
-__device__ __noinline__ Scales load_odd_scales(const uint8_t* p, int bytes) {
-    Scales v;
-#pragma unroll 1
-    for (int i = 0; i < 8; i++) {
-        unsigned w = 0x7f7f7f7f;
-        if (4 * i + 4 <= bytes && ((uintptr_t)p & 3) == 0) w = *(const unsigned*)(p + 4 * i);
-        else
-            for (int b = 0; b < 4; b++)
-                if (4 * i + b < bytes) w = (w & ~(255u << (8 * b))) | (unsigned)p[4 * i + b] << (8 * b);
-        v.w[i] = w;
-    }
-    return v;
-}
-__device__ __forceinline__ Scales load_scales(const uint8_t* row, int k, int bytes, bool there) {
-    Scales v;
-    const uint8_t* const p = row + k;
-    const bool whole = k + 32 <= bytes;
-    if (there && whole && ((uintptr_t)p & 31) == 0) {                 // a sector at once: every part of it is a request to L2 of its own
-        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7]) : "l"(p));
-    } else if (there && whole && ((uintptr_t)p & 15) == 0) {
-        const uint4 a = *(const uint4*)p, b = *(const uint4*)(p + 16);
-        v = Scales{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-    } else if (there) {
-        v = load_odd_scales(p, min(bytes - k, 32));
-    } else {
+// n[j] scales from p[j], any alignment, and 1 behind them: whole words around them (a word that holds one of them is inside the same memory),
+// shifted into place.  All loads before the first use; out of line: inside the loop of every loader it cost instruction cache.
+__device__ __noinline__ void load_odd_scales(const uint8_t* const (&p)[4], const int (&n)[4], Scales (&v)[4]) {
+    unsigned w[4][9];
 #pragma unroll
-        for (int i = 0; i < 8; i++) v.w[i] = 0x7f7f7f7f;
+    for (int j = 0; j < 4; j++) {
+        const int off = (int)((uintptr_t)p[j] & 3);
+#pragma unroll
+        for (int i = 0; i < 9; i++) w[j][i] = 4 * i - off < n[j] ? *(const unsigned*)(p[j] - off + 4 * i) : 0;
     }
-    return v;
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const unsigned x = __funnelshift_r(w[j][i], w[j][i + 1], 8 * ((uintptr_t)p[j] & 3));
+            const int left = n[j] - 4 * i;
+            const unsigned keep = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1);
+            v[j].w[i] = (x & keep) | (0x7f7f7f7fu & ~keep);
+        }
+}
+// 32 scales of four rows from byte k of rows of `bytes`; 1 behind their ends and in rows that are not there.
+__device__ __forceinline__ void load_scales(const uint8_t* const (&row)[4], const bool (&there)[4], int k, int bytes, int aligned, Scales (&v)[4]) {
+    if (k + 32 <= bytes && aligned >= 16) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint8_t* const p = row[j] + k;
+            if (there[j] && aligned == 32) {      // a sector at once: every part of it is a request to L2 of its own
+                asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(v[j].w[0]), "=r"(v[j].w[1]), "=r"(v[j].w[2]), "=r"(v[j].w[3]), "=r"(v[j].w[4]), "=r"(v[j].w[5]),
+                               "=r"(v[j].w[6]), "=r"(v[j].w[7]) : "l"(p));
+            } else if (there[j]) {
+                const uint4 a = *(const uint4*)p, b = *(const uint4*)(p + 16);
+                v[j] = Scales{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i++) v[j].w[i] = 0x7f7f7f7f;
+            }
+        }
+        return;
+    }
+    const uint8_t* p[4];
+    int n[4];
+    Scales odd[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        p[j] = row[j] + k;
+        n[j] = there[j] ? min(bytes - k, 32) : 0;
+    }
+    load_odd_scales(p, n, odd);
+#pragma unroll
+    for (int j = 0; j < 4; j++) v[j] = odd[j];
 }
 
 template <int CG, typename T>
@@ -232,6 +252,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     __shared__ unsigned s_tmem;
     __shared__ int s_n, s_most;
     __shared__ volatile int s_stop;
+    static_assert(3 * S::most_stages + 5 <= 64, "a thread per barrier");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x % CG);          // of the pair
     const unsigned base = (smem_u32(s_raw) + 1023) & ~1023u;
@@ -246,18 +267,16 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     const auto done = [&](int b) { return bars3 + 8 * b; };                                 // of each: a tile is summed
     const auto free_ = [&](int b) { return bars3 + 8 * (2 + b); };                          // of the first: its columns may be used again
     const unsigned drained = bars3 + 32;
-    if (tid == 0) {
-        for (int s = 0; s < S::most_stages; s++) {
-            mbar_init(full(s), 2 * CG);           // per CTA: the operands' loader, and warp 9 for the scales
-            mbar_init(empty(s), 1);
-            mbar_init(written(s), 1 + CG);
-        }
-        for (int b = 0; b < 2; b++) {
-            mbar_init(done(b), 1);
-            mbar_init(free_(b), 4 * CG);
-        }
-        mbar_init(drained, 1);
+    if (tid < 3 * S::most_stages + 5) {           // a barrier each
+        const int i = tid / S::most_stages, last = tid - 3 * S::most_stages;
+        // (full: per CTA the operands' loader, and warp 9 for the scales)
+        const int arrivals = last >= 0 ? (last == 2 || last == 3 ? 4 * CG : 1) : (i == 0 ? 2 * CG : (i == 1 ? 1 : 1 + CG));
+        mbar_init(bars + 8 * tid, arrivals);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    } else if (tid >= 64 && tid < 68) {
+        const CUtensorMap* const maps[4] = {&x_map, &x_64_map, &x_32_map, &w_map};
+        asm volatile("prefetch.tensormap [%0];" ::"l"(maps[tid - 64]) : "memory");
+    } else if (tid == 96) {
         s_stop = 0;
     }
     if (warp == 1) {
@@ -413,18 +432,21 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
         const bool is_b = warp != 2;
         const int half = warp == 8 ? 1 : 0, bytes = a.K / 32, chunks = (k_tiles + 3) / 4;
         const unsigned to = (is_b ? S::sa_bytes + 512 * half : 0) + lane * 16, word_step = is_b ? 512 * CG : 512;
+        const unsigned long long border = is_b ? (uintptr_t)a.ws | (unsigned long long)bytes : (uintptr_t)a.xs | (unsigned long long)a.xs_ld;
+        const int aligned = border % 32 == 0 ? 32 : (border % 16 == 0 ? 16 : 1);
         Tile tile{};
         const auto load = [&](long long t, int chunk, Scales (&v)[4]) {
             if (t >= tiles) return;
             if (chunk == 0) tile = tile_of(a, ex, t, n_tiles, MT, NT);
+            const uint8_t* row[4];
+            bool there[4];
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 const int r = lane + 32 * j + (is_b ? 128 * half : kPrM * rank);
-                const bool there = is_b ? tile.n0 + r < a.F : r < tile.rows;
-                const uint8_t* const row = is_b ? a.ws + ((long long)tile.e * a.F + tile.n0 + r) * bytes
-                                                : a.xs + (long long)(tile.first + r) * a.xs_ld;
-                v[j] = load_scales(row, chunk * 32, bytes, there);
+                there[j] = is_b ? tile.n0 + r < a.F : r < tile.rows;
+                row[j] = is_b ? a.ws + ((long long)tile.e * a.F + tile.n0 + r) * bytes : a.xs + (long long)(tile.first + r) * a.xs_ld;
             }
+            load_scales(row, there, chunk * 32, bytes, aligned, v);
         };
         Scales next[4], v[4];
         load(t0, 0, next);

@@ -261,6 +261,21 @@ def test_product_of_contiguous_rows_and_offsets_that_do_not_begin_at_zero(vp):
         _check(vp, _operands([9, 0, 50], 130, K, K, spare=70, first=13), torch.float32, wire=False)
 
 
+@pytest.mark.parametrize("K", [32, 416, 1024, 1056, 2080])
+def test_product_of_scales_at_any_alignment(vp, K):
+    """Rows of scales that begin at every byte of a sector and are any number of bytes apart; what lies around them is NaN."""
+    o = _operands([130, 1, 30], 40, K, K)
+    want, size = _expected(o)
+    n = K // 32
+    for first, width in ((0, n + 77), (1, n + 77), (2, n + 5), (3, n + 1), (16, n + 16), (29, n + 32)):
+        flat = torch.full((162 * (n + 77),), 255, dtype=torch.uint8, device="cuda")
+        scales = torch.as_strided(flat, (161, n), (width, 1), first)
+        scales.copy_(o["xs"])
+        out = torch.zeros(161, 40, device="cuda")
+        vp.mxfp4_product(o["xc"].cuda(), scales, o["wc"].cuda(), o["ws"].cuda(), o["off"].cuda(), out)
+        assert ((out.cpu().double() - want).abs() <= _bound(o, size, want, torch.float32)).all()
+
+
 def test_product_of_a_thousand_experts(vp):
     g = _gen(6)
     counts = (torch.rand(1024, generator=g) < 0.3).long() * torch.randint(1, 4, (1024,), generator=g)
