@@ -10,8 +10,8 @@
 // logits are compared.  With one, 32-bit keys are computed with a bound on their error; where two keys that matter are nearer
 // than twice that bound and do not come from equal logits and biases, those are compared in 64 bits (one token in some 400).
 //
-// Bound by instructions: about 750 a token of 256 experts, of which a quarter are the scores.  16,384 tokens x 256 fp32 logits, sigmoid, bias, best
-// 8 of 4 of 8 groups: 16.6 us (41 with all keys of an unclear token in 64 bits and one expert chosen per round), where reading the
+// Bound by instructions: about 760 a token of 256 experts, of which a quarter are the scores.  16,384 tokens x 256 fp32 logits, sigmoid, bias, best
+// 8 of 4 of 8 groups: 16.0 us (41 with all keys of an unclear token in 64 bits and one expert chosen per round), where reading the
 // logits takes 2.7; 128 tokens 3.4 us, a launch and one warp's chain.
 #include <cmath>
 #include <type_traits>
@@ -32,7 +32,7 @@ struct RouteArgs {
     const float* bias;
     bool sigmoid, renormalise, wide, wide_bias;   // wide: rows can be loaded by vectors
     int n_group, topk_group, group_top, per;      // per: experts of a group
-    int lanes_per_group;                          // a power of two when groups are whole lanes', else 0
+    int lanes_per_group, group_shift;             // 2^group_shift when groups are that many whole lanes', else 0
     float scale;
     int32_t* idx;
     float* weights;
@@ -63,7 +63,7 @@ __device__ __forceinline__ void load_logits(const T* row, int E, bool wide, floa
     for (int v = 0; v < VPL; v++) z[v] = logit_of(value_of(raw[v]));
 }
 
-// Biases of experts lane * VPL .., 0 without one; -inf keeps an expert from being chosen.
+// Biases of experts lane * VPL .. as they are, 0 without one.
 template <int VPL>
 __device__ __forceinline__ void load_bias(const float* bias, int E, bool wide, float (&b)[VPL]) {
     constexpr int V = VPL % 4 == 0 ? 4 : (VPL % 2 == 0 ? 2 : 1);
@@ -73,10 +73,10 @@ __device__ __forceinline__ void load_bias(const float* bias, int E, bool wide, f
         if (wide && first + v + V <= E) {
             const Pack<float, V> p = *(const Pack<float, V>*)(bias + first + v);
 #pragma unroll
-            for (int u = 0; u < V; u++) b[v + u] = logit_of(p.v[u]);
+            for (int u = 0; u < V; u++) b[v + u] = p.v[u];
         } else {
 #pragma unroll
-            for (int u = 0; u < V; u++) b[v + u] = bias && first + v + u < E ? logit_of(bias[first + v + u]) : 0.f;
+            for (int u = 0; u < V; u++) b[v + u] = bias && first + v + u < E ? bias[first + v + u] : 0.f;
         }
     }
 }
@@ -227,8 +227,8 @@ route_kernel(const __grid_constant__ RouteArgs a) {
     __shared__ int s_at[kRouteWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = lane * VPL;
     grid_wait();
-    const long long t = (long long)blockIdx.x * (blockDim.x >> 5) + warp;
-    if (t >= a.T) return;
+    const int t = (int)(blockIdx.x * (blockDim.x >> 5)) + warp;
+    if ((unsigned)t >= (unsigned)a.T) return;     // (the last CTA's warps may pass 2^31)
     const T* const row = (const T*)a.logits + t * a.ld;
     float z[VPL], key[VPL];
     load_logits<T, VPL>(row, a.E, a.wide, z);
@@ -258,11 +258,11 @@ route_kernel(const __grid_constant__ RouteArgs a) {
         for (int v = 0; v < VPL; v++) {
             const float k = (a.sigmoid ? reciprocal(1 + fast_exp(-z[v])) : fast_exp(z[v] - most) * over) + b[v];
             largest = fmaxf(largest, fabsf(k));
-            by[v] = z[v] > -CUDART_INF_F ? k : -CUDART_INF_F;
+            by[v] = z[v] > -CUDART_INF_F ? fmaxf(k, -CUDART_INF_F) : -CUDART_INF_F;      // (NaN of the bias: -inf)
             if (rounded_keys) key[v] = by[v];
         }
         largest = warp_max(largest);
-        if (!(largest < CUDART_INF_F)) {          // a bias of -inf, or no logit
+        if (!(largest < CUDART_INF_F)) {          // a bias of -inf (or inf: then all keys are compared in 64 bits), or no logit
             largest = 0;
 #pragma unroll
             for (int v = 0; v < VPL; v++)
@@ -314,7 +314,7 @@ route_kernel(const __grid_constant__ RouteArgs a) {
             }
         }
         if (a.lanes_per_group) {
-            const bool shut = !(open >> (lane / a.lanes_per_group) & 1);
+            const bool shut = !(open >> (lane >> a.group_shift) & 1);
 #pragma unroll
             for (int v = 0; v < VPL; v++)
                 if (shut) key[v] = -CUDART_INF_F;
@@ -421,8 +421,9 @@ route_kernel(const __grid_constant__ RouteArgs a) {
         w = sum > 0 ? w * reciprocal(sum) : 0.f;
     }
     if (lane < a.topk) {
-        a.idx[t * a.topk + lane] = chosen;
-        a.weights[t * a.topk + lane] = w * a.scale;
+        const int at = t * a.topk + lane;         // (below 2^31 in all)
+        a.idx[at] = chosen;
+        a.weights[at] = w * a.scale;
     }
 }
 
@@ -571,6 +572,8 @@ extern "C" int vp_route(const vp_route_params* p, const void* logits, int dtype,
             constexpr int n = decltype(vpl)::value;
             const int lanes = a.per % n ? 0 : a.per / n;
             a.lanes_per_group = lanes > 0 && (lanes & (lanes - 1)) == 0 && a.n_group * lanes <= 32 ? lanes : 0;
+            a.group_shift = 0;
+            while (1 << a.group_shift < a.lanes_per_group) a.group_shift++;
             const size_t smem = a.n_group > 1 && !a.lanes_per_group ? (size_t)warps * a.E * 4 : 0;
             e = launch_after(route_kernel<X, n>, grid, warps * 32, smem, (cudaStream_t)cuda_stream, a);
         });
