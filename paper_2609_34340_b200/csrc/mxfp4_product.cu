@@ -16,7 +16,7 @@
 // What bounds it: with few rows per expert HBM, by which the matrices come (16 experts x 4,096 x 7,168, 128 rows: 48 us, 5.2 TB/s; without the loads of
 // scales 43, so a seventh is their latency); with many the operands' way from L2 to the SMs, 11 TB/s here (16,384 rows, 8 experts, 7,168 x 4,096: 175 us,
 // 5.5 PFLOP/s; the loads alone 176, the products alone 122); a single row is a chain of a third of a microsecond per 256 values of k
-// (7,168 x 4,096: 12.7 us).  Tried: scales through asynchronous copies to shared memory, or two to four chunks ahead in registers (1.1 to 1.5 times the
+// (7,168 x 4,096: 12 us).  Tried: scales through asynchronous copies to shared memory, or two to four chunks ahead in registers (1.1 to 1.5 times the
 // time), scales in tensor memory a stage ahead with barriers of their own (1.4 times), one CTA on 128 x 256 (274 us).
 #include <cuda.h>
 #include <type_traits>
