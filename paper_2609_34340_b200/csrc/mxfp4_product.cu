@@ -73,6 +73,9 @@ __device__ __forceinline__ unsigned in_cta(unsigned at, unsigned rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(rank));
     return r;
 }
+// Arrivals at the other CTA's barriers carry order only, no data: what a stage holds is read by the SM that holds it, after a proxy fence in
+// that SM, and tensor memory is ordered by the tcgen05 fences.  With release and acquire of the cluster's scope, in every arrival and poll,
+// the product of 16,384 rows, 7,168 x 4,096, took 439 us instead of 252.
 __device__ __forceinline__ void cluster_arrive(unsigned bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
