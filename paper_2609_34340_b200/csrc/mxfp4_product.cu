@@ -23,6 +23,7 @@
 
 #include "bulk_copy.cuh"
 #include "elements.cuh"
+#include "odd_words.h"
 
 namespace {
 
@@ -191,25 +192,20 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a, const Experts& x, 
 
 // 32 scales of a row.
 struct Scales { unsigned w[8]; };
-// n[j] scales from p[j], any alignment, and 1 behind them: whole words around them (a word that holds one of them is inside the same memory),
-// shifted into place.  All loads before the first use; out of line: inside the loop of every loader it cost instruction cache.
+// n[j] scales from p[j], any alignment, and 1 behind them.  All loads before the first use; out of line: inside the loop of every loader it
+// cost instruction cache.
 __device__ __noinline__ void load_odd_scales(const uint8_t* const (&p)[4], const int (&n)[4], Scales (&v)[4]) {
     unsigned w[4][9];
 #pragma unroll
     for (int j = 0; j < 4; j++) {
         const int off = (int)((uintptr_t)p[j] & 3);
 #pragma unroll
-        for (int i = 0; i < 9; i++) w[j][i] = 4 * i - off < n[j] ? *(const unsigned*)(p[j] - off + 4 * i) : 0;
+        for (int i = 0; i < 9; i++) w[j][i] = odd_word_holds(i, off, n[j]) ? *(const unsigned*)(p[j] - off + 4 * i) : 0;
     }
 #pragma unroll
     for (int j = 0; j < 4; j++)
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const unsigned x = __funnelshift_r(w[j][i], w[j][i + 1], 8 * ((uintptr_t)p[j] & 3));
-            const int left = n[j] - 4 * i;
-            const unsigned keep = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1);
-            v[j].w[i] = (x & keep) | (0x7f7f7f7fu & ~keep);
-        }
+        for (int i = 0; i < 8; i++) v[j].w[i] = odd_word(w[j][i], w[j][i + 1], i, (int)((uintptr_t)p[j] & 3), n[j], 0x7f7f7f7fu);
 }
 // 32 scales of four rows from byte k of rows of `bytes`; 1 behind their ends and in rows that are not there.
 __device__ __forceinline__ void load_scales(const uint8_t* const (&row)[4], const bool (&there)[4], int k, int bytes, int aligned, Scales (&v)[4]) {

@@ -217,3 +217,30 @@ int main() {
     assert(!pinned_address(p, 2 * K));
 }
 ''')
+
+
+def test_words_around_a_run_of_bytes(tmp_path):
+    """Scales of a row at any address are read by whole words: every word that is read holds a byte of the row (none for a row that is not
+    there, whose address is nobody's memory), and the bytes come out in order with the fill behind them."""
+    _run(tmp_path, r'''
+#include "odd_words.h"
+int main() {
+    for (int off = 0; off < 4; off++)
+        for (int n = 0; n <= 32; n++) {
+            uint32_t w[9];
+            for (int i = 0; i < 9; i++) {
+                const int first = 4 * i - off;                       // of the word's bytes, counted from the run's first
+                const bool holds = n > 0 && first < n && first + 4 > 0;
+                assert(odd_word_holds(i, off, n) == holds);
+                w[i] = holds ? 0 : 0xEEEEEEEEu;
+                for (int b = 0; holds && b < 4; b++)
+                    w[i] |= (uint32_t)(first + b >= 0 && first + b < n ? first + b + 1 : 0xEE) << (8 * b);
+            }
+            for (int i = 0; i < 8; i++)
+                for (int b = 0; b < 4; b++) {
+                    const uint32_t want = 4 * i + b < n ? 4 * i + b + 1 : 0x7f;
+                    assert((odd_word(w[i], w[i + 1], i, off, n, 0x7f7f7f7fu) >> (8 * b) & 255) == want);
+                }
+        }
+}
+''')
