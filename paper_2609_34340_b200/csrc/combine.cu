@@ -195,7 +195,7 @@ combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
         if (warp > 0) return;
         for (int k = 0; k < kGradShared / 32 && lane < S; k++) mine += s_part[k][lane];
     }
-    if (lane < slots) a.grad_weights[first + lane] = mine;
+    if (lane < slots) a.grad_weights[first + lane] = at >= 0 ? mine : 0.f;      // (a dropped copy's zeros times an infinity are not 0)
 }
 
 // The same value by value, for rows that do not begin on 16-byte borders.

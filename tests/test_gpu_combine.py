@@ -71,6 +71,24 @@ def test_combine_backward_matches_the_definition(vp, T, topk, H, dtype):
     assert torch.equal(only_rows, grad_rows) and torch.equal(only_weights, grad_weights)
 
 
+@pytest.mark.parametrize("T,topk,H,first", [(5, 6, 96, 0), (30, 4, 1032, 0), (700, 8, 1032, 0), (3, 8, 4104, 0), (2, 11, 8200, 0), (6, 3, 50, 0), (9, 5, 64, 1)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_dropped_copies_have_no_gradient_whatever_the_tokens_gradient_holds(vp, T, topk, H, first, dtype):
+    """An overflowed step: infinities and NaN in the gradient of tokens with dropped copies.  Short rows, long rows, rows of many tokens, rows
+    that do not begin on 16-byte borders (first: values in front of them)."""
+    idx, w, rows, grad = _case(T, topk, H, dtype, T + H, dropped=0.5)
+    idx[0, 0], idx[0, 1] = 3, -1
+    rows = torch.where((idx >= 0).view(-1, 1), torch.ones_like(rows), rows)
+    grad[0, H // 2] = math.inf
+    grad[2 % T, H - 1] = math.nan
+    grad[T - 1, 0] = -math.inf
+    flat = torch.zeros(T * topk * H + first, dtype=dtype, device="cuda")[first:].view(T * topk, H)
+    flat.copy_(rows)
+    grad_rows, grad_weights = (t.cpu() for t in vp.combine_backward(grad.cuda(), flat, idx.cuda(), w.cuda()))
+    assert (grad_weights[idx < 0] == 0).all() and (grad_rows[(idx < 0).view(-1)] == 0).all()
+    assert torch.equal(torch.isfinite(grad_weights), (idx < 0) | torch.isfinite(grad).all(dim=1, keepdim=True))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_combine_backward_matches_differences(vp, dtype):
     """The sum is linear in rows and in weights: a difference is the derivative up to rounding."""
