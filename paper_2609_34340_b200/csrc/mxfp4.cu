@@ -94,15 +94,25 @@ __device__ __forceinline__ unsigned codes_of(const float (&x)[8]) {
     return r;
 }
 
-// x / (1 + e^-x).  e^-x = 2^t with t = -x log2 e: what the product t loses is added to the first order, so that the exponential is off by
-// 2^-21, the whole by four units in the last place at most, whatever x (0 from -88 on, where e^-x leaves 32 bits).
+// x / (1 + e^-x) over all of x: off by five units in the last place at most (a result below the normal numbers: by half of their smallest
+// step); 0 times x where the exponential outgrows any x.
+//   e^-x = 2^t, t = -x log2 e.  log2 e is split into its 32-bit value and the rest (the reduction of Cody and Waite); what the product t loses
+//   is added to the first order, so that the exponential is off by little more than its own 2^-22.
+//   x is held within +-132.5 for the exponential, which keeps t and its rest finite; it is 0 or 2^127.2 times its scale at the ends.
+//   From t = 96 on, where 1 + e^-x = e^-x, the exponential is that of t - 64 (an exact difference), so that neither it nor its reciprocal
+//   leaves the normal numbers before the result does; the result is scaled by 2^-64 then.
+constexpr double kLog2e = 1.4426950408889634;
+constexpr float kLog2eHigh = (float)kLog2e, kLog2eRest = (float)(kLog2e - (double)kLog2eHigh);
 __device__ __forceinline__ float silu(float x) {
-    const float t = x * -1.4426950408889634f, rest = fmaf(x, -1.4426950408889634f, -t) - x * 1.925963033e-8f;
+    const float near = fminf(fmaxf(x, -132.5f), 132.5f), t = near * -kLog2eHigh;
+    const float rest = fmaf(near, -kLog2eRest, fmaf(near, -kLog2eHigh, -t));
+    const bool far = t > 96;
     float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-    if (e < CUDART_INF_F) e = fmaf(e, rest * 0.6931471805599453f, e);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(far ? t - 64 : t));
+    e = fmaf(e, rest * 0.6931471805599453f, e);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1 + e));
-    return x * r;
+    const float y = x * r;
+    return far ? y * 5.421010862427522e-20f : y;
 }
 
 // 2^e, -127 <= e <= 127.

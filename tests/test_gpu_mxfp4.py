@@ -141,6 +141,52 @@ def test_gated_quantize(vp, R, K, dtype):
     assert clear.double().mean() > 0.99
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("far", [0, 1, 2])
+def test_gated_quantize_over_the_whole_range_of_gates(vp, dtype, far):
+    """A gate to a block, from the type's lowest value to its largest, both sides of -87.3 (where 1 + e^-x passes 2^126) and -88.7 (where e^-x
+    leaves 32 bits), down to where the activation vanishes, infinities and NaN; times factors that bring it to every place between two codes.
+    The activation is off by five units in the last place (an exponential 2, its correction, the sum and the product half a one each, the reciprocal 1)
+    and its product with the factor by half a one, and what is not a normal number by half the smallest step, so the code is that of a value
+    within these."""
+    top = torch.finfo(dtype).max
+    gates = torch.tensor([top, -top, top * 0.7, -top * 0.7, top / 4, 2.36e38, 2.37e38, -2.37e38, 1e30, -1e30, 130.0, 133.0, -130.0, -133.0, -200.0, -60.0,
+                          -64.5, -66.0, -67.5, -87.0, -87.25, -87.5, -88.0, -88.5, -88.75, -89.0, -91.0, -95.0, -100.0, -104.0, -110.0, 87.5, 89.0, 40.0,
+                          0.0, -0.0, 1e-30, -1e-30, 2.0 ** -20, -1.0, 1.0, -16.0, 16.0, -17.5, math.inf, -math.inf, math.nan], dtype=torch.float32)
+    gates = torch.cat([gates[gates.abs() <= top], gates[-3:]]).to(dtype)
+    up = torch.linspace(0.51, 0.99, 32).to(dtype) * (2.0 ** [0, -60 if dtype != torch.float16 else -4, 40 if dtype != torch.float16 else 10][far])
+    h = torch.cat([gates.view(-1, 1).expand(-1, 32), up.to(dtype).expand(len(gates), 32)], dim=1).contiguous()
+    codes, scales = (t.cpu() for t in vp.mxfp4_quantize(h.cuda(), gated=True))
+    gate, f = h[:, :32].double(), h[:, 32:].double()
+    a = gate / (1 + torch.exp(-gate))                 # (e^-x of 64 bits does not overflow before -709)
+    a = torch.where(gate < -700, gate * 0, a)
+    off, least = 5 * 2.0 ** -23, 2.0 ** -150
+    lo, hi = a - (a.abs() * off + least), a + (a.abs() * off + least)
+    lo, hi = lo * f, hi * f                           # (f > 0)
+    lo, hi = lo - (lo.abs() * 2.0 ** -24 + least), hi + (hi.abs() * 2.0 ** -24 + least)
+    beyond = torch.finfo(torch.float32).max
+    bad = ~torch.isfinite(a * f).all(dim=1) | ((a * f).abs() > beyond).any(dim=1)
+    assert torch.equal(scales.view(-1) == 255, bad) and (codes[bad] == 0).all() and int(bad.sum()) >= 3
+    got = ref.decode(codes, scales)
+    for r in torch.nonzero(~bad).view(-1).tolist():
+        # The scale is one of those between the least and the largest magnitude that the block can have; under it the codes lie between the ends'.
+        least_of = torch.where((lo[r] <= 0) & (hi[r] >= 0), 0.0, torch.minimum(lo[r].abs(), hi[r].abs()))
+        ends = [float(m.max()) for m in (least_of, torch.maximum(lo[r].abs(), hi[r].abs()))]
+        want = [max(math.frexp(m)[1] - 3, -127) if m > 0 else -127 for m in ends]
+        e = int(scales[r, 0]) - 127
+        assert want[0] <= e <= want[1], (float(gates[r]), e, want)
+        step = 2.0 ** e
+        at = [torch.tensor([_nearest(float(v) / step) for v in x[r]], dtype=torch.float64) * step for x in (lo, hi)]
+        assert ((at[0] <= got[r]) & (got[r] <= at[1])).all(), float(gates[r])
+
+
+def _nearest(x):
+    """The value of the grid next to x: ties to even, magnitudes above 6 to 6."""
+    a = min(abs(x), 6.0)
+    step = 0.5 if a < 2 else (1.0 if a < 4 else 2.0)
+    return math.copysign(round(a / step) * step, x)       # (Python rounds ties to even; a grid point's code is even where its quotient is)
+
+
 def test_quantize_refuses(vp):
     x = torch.zeros(4, 64, device="cuda")
     codes, scales = torch.zeros(4, 32, dtype=torch.uint8, device="cuda"), torch.zeros(4, 2, dtype=torch.uint8, device="cuda")
