@@ -95,24 +95,25 @@ __device__ __forceinline__ unsigned codes_of(const float (&x)[8]) {
 }
 
 // x / (1 + e^-x) over all of x: off by five units in the last place at most (a result below the normal numbers: by half of their smallest
-// step); 0 times x where the exponential outgrows any x.
-//   e^-x = 2^t, t = -x log2 e.  log2 e is split into its 32-bit value and the rest (the reduction of Cody and Waite); what the product t loses
-//   is added to the first order, so that the exponential is off by little more than its own 2^-22.
-//   x is held within +-132.5 for the exponential, which keeps t and its rest finite; it is 0 or 2^127.2 times its scale at the ends.
-//   From t = 96 on, where 1 + e^-x = e^-x, the exponential is that of t - 64 (an exact difference), so that neither it nor its reciprocal
-//   leaves the normal numbers before the result does; the result is scaled by 2^-64 then.
+// step as well).
+//   e^-x = 2^n 2^f with n an integer next to -x log2 e (found by adding 1.5 * 2^23, which leaves no bits behind the point) and f the rest, in
+//   two steps with log2 e split into its 32-bit value and what that lacks (the reduction of Cody and Waite).
+//   1 / (1 + 2^n 2^f) = 2^-n / (2^-n + 2^f): nothing leaves the normal numbers before the result does.
+//   n is held within -30 (the sum is 1 from there on) and 126 by a product that saturates; f takes what is beyond, up to an infinity, whose
+//   reciprocal is 0.
 constexpr double kLog2e = 1.4426950408889634;
 constexpr float kLog2eHigh = (float)kLog2e, kLog2eRest = (float)(kLog2e - (double)kLog2eHigh);
 __device__ __forceinline__ float silu(float x) {
-    const float near = fminf(fmaxf(x, -132.5f), 132.5f), t = near * -kLog2eHigh;
-    const float rest = fmaf(near, -kLog2eRest, fmaf(near, -kLog2eHigh, -t));
-    const bool far = t > 96;
+    constexpr float whole = 12582912, least = -30, range = 156;
+    float held;
+    asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(held) : "f"(x), "f"((float)(-kLog2e / range)), "f"(-least / range));
+    const float m = fmaf(held, range, whole + least);
+    const float f = fmaf(x, -kLog2eRest, fmaf(x, -kLog2eHigh, whole - m));
+    const float down = __uint_as_float(__float_as_uint(m) * (0u - (1u << 23)) + (127u << 23));      // 2^-n (the bits of m end in those of n)
     float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(far ? t - 64 : t));
-    e = fmaf(e, rest * 0.6931471805599453f, e);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1 + e));
-    const float y = x * r;
-    return far ? y * 5.421010862427522e-20f : y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(down + e));
+    return x * r * down;
 }
 
 // 2^e, -127 <= e <= 127.
