@@ -108,9 +108,13 @@ __device__ __forceinline__ void merge(K& hi, K& lo, K hi2, K lo2) {
     lo = larger(larger(lo, lo2), smaller(hi, hi2));
     hi = larger(hi, hi2);
 }
+// What a group is judged by; -inf only where it has nothing to choose.  Two keys of the lowest value, an expert's bias where it is kept out that
+// way, add up to less than 32 bits hold: held there, such groups are equal, and compared in 64 bits.
+__device__ __forceinline__ float within(float x) { return fminf(fmaxf(x, -CUDART_MAX_NORMAL_F), CUDART_MAX_NORMAL_F); }
+__device__ __forceinline__ double within(double x) { return x; }
 template <typename K>
 __device__ __forceinline__ K sum_of_two(K a, K b, int top) {
-    return top > 1 && b > -(K)CUDART_INF_F ? a + b : a;
+    return top > 1 && b > -(K)CUDART_INF_F ? within(a + b) : a;
 }
 
 // What a softmax score in 64 bits is taken from: the largest logit and the sum of the exponentials below it.

@@ -111,6 +111,26 @@ def test_route_of_masked_experts_and_empty_rows(vp, scoring, with_bias, n_group,
 
 
 @pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,n_group,topk_group,topk", [(32, 4, 2, 12), (60, 4, 2, 20), (60, 4, 3, 32), (256, 8, 4, 32), (1000, 5, 2, 32)])
+def test_route_of_biases_of_the_lowest_value(vp, scoring, experts, n_group, topk_group, topk):
+    """Experts kept out by the type's lowest value instead of -inf: they can still be chosen, after all others, and so can groups of
+    nothing else, whose two best keys add up to less than 32 bits hold."""
+    g = _gen(experts + topk)
+    p = vp.RouteParams(experts, topk, scoring, n_group, topk_group, 2, True, 1.0)
+    z = torch.randn(24, experts, generator=g)
+    z[3] = -math.inf
+    per, low = experts // n_group, torch.finfo(torch.float32).min
+    for open_ in ([0], [n_group - 1], [], [1, 2], list(range(n_group))):
+        bias = torch.full((experts,), low)
+        for group in open_:
+            bias[group * per:(group + 1) * per] = torch.randn(per, generator=g) * 0.05
+        if len(open_) == n_group:
+            bias[1::3] = low
+            bias[:per] = torch.finfo(torch.float32).max
+        _check(vp, p, z, bias)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("n_group,topk_group,group_top", [(1, 1, 1), (8, 4, 2)])
 def test_route_of_equal_logits_takes_the_lowest_index(vp, scoring, n_group, topk_group, group_top):
     p = vp.RouteParams(256, 8, scoring, n_group, topk_group, group_top, True, 1.0)
