@@ -518,6 +518,7 @@ def unpack_tokens(plan: Plan, b: int, rank: int, expert_idx: torch.Tensor, exper
 
 
 # ---- around the AlltoAllv: router, weighted sum, 4-bit rows, the experts' products ------------------------------------------
+# (what these calls allocate themselves belongs to the stream that they run on)
 
 @dataclass
 class RouteParams:
@@ -532,15 +533,24 @@ class RouteParams:
     scale: float = 1.0
 
 
+def _alloc(make, shape, dtype, device, stream):
+    """What a call on ``stream`` writes, allocated (and cleared) there: memory of the current stream may still be written by what that one
+    has not run yet."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device)):
+        return make(shape, dtype=dtype, device=device)
+
+
 def route(params: RouteParams, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, expert_idx: Optional[torch.Tensor] = None,
           weights: Optional[torch.Tensor] = None, stream=None):
     """``vp_route``: the experts and weights of ``[T, experts]`` router logits (bfloat16, float16 or float32).  Returns
     ``(expert_idx, weights)``, int32 and float32 ``[T, topk]``: what :func:`demand_from_routing`, :func:`pack` and
     :func:`combine` take.  Not differentiable by itself: see :func:`route_backward`."""
     if expert_idx is None:
-        expert_idx = torch.empty((logits.shape[0], params.topk), dtype=torch.int32, device=logits.device)
+        expert_idx = _alloc(torch.empty, (logits.shape[0], params.topk), torch.int32, logits.device, stream)
     if weights is None:
-        weights = torch.empty((logits.shape[0], params.topk), dtype=torch.float32, device=logits.device)
+        weights = _alloc(torch.empty, (logits.shape[0], params.topk), torch.float32, logits.device, stream)
     rc = (_calls or _load_calls()).route(params, logits, bias, expert_idx, weights, stream)
     if rc:
         _check(rc, "vp_route")
@@ -551,7 +561,7 @@ def route_backward(params: RouteParams, logits: torch.Tensor, expert_idx: torch.
                    grad_logits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """``vp_route_backward``: gradient of the weights with respect to the logits, for the choice ``expert_idx``."""
     if grad_logits is None:
-        grad_logits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        grad_logits = _alloc(torch.empty, logits.shape, logits.dtype, logits.device, stream)
     rc = (_calls or _load_calls()).route_backward(params, logits, expert_idx, grad_weights, grad_logits, stream)
     if rc:
         _check(rc, "vp_route_backward")
@@ -563,7 +573,7 @@ def combine(rows: torch.Tensor, expert_idx: torch.Tensor, weights: torch.Tensor,
     """``vp_combine``: ``base[t] + sum_s weights[t, s] * rows[t * topk + s]`` over the slots with ``expert_idx >= 0``; ``rows``
     ``[T * topk, H]`` as :func:`unpack_tokens` writes them."""
     if out is None:
-        out = torch.empty((expert_idx.shape[0], rows.shape[1]), dtype=rows.dtype, device=rows.device)
+        out = _alloc(torch.empty, (expert_idx.shape[0], rows.shape[1]), rows.dtype, rows.device, stream)
     rc = (_calls or _load_calls()).combine(rows, expert_idx, weights, base, out, stream)
     if rc:
         _check(rc, "vp_combine")
@@ -574,9 +584,9 @@ def combine_backward(grad: torch.Tensor, rows: torch.Tensor, expert_idx: torch.T
                      grad_rows: Optional[torch.Tensor] = None, grad_weights: Optional[torch.Tensor] = None, stream=None):
     """``vp_combine_backward``: returns ``(grad_rows, grad_weights)`` for the gradient ``[T, H]`` of :func:`combine`'s result."""
     if grad_rows is None:
-        grad_rows = torch.empty(rows.shape, dtype=rows.dtype, device=rows.device)
+        grad_rows = _alloc(torch.empty, rows.shape, rows.dtype, rows.device, stream)
     if grad_weights is None:
-        grad_weights = torch.empty(weights.shape, dtype=torch.float32, device=rows.device)
+        grad_weights = _alloc(torch.empty, weights.shape, torch.float32, rows.device, stream)
     rc = (_calls or _load_calls()).combine_backward(grad, rows, expert_idx, weights, grad_rows, grad_weights, stream)
     if rc:
         _check(rc, "vp_combine_backward")
@@ -601,7 +611,7 @@ def mxfp4_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales
     if codes is None or scales is None:
         cols = x.shape[1] // (2 if gated else 1)
         assert codes is None and scales is None and cols % 32 == 0, "codes and scales: both or none, for rows of whole blocks of 32 values"
-        codes, scales = mxfp4_rows(torch.empty((x.shape[0], mxfp4_row_bytes(cols)), dtype=torch.uint8, device=x.device), cols)
+        codes, scales = mxfp4_rows(_alloc(torch.empty, (x.shape[0], mxfp4_row_bytes(cols)), torch.uint8, x.device, stream), cols)
     rc = (_calls or _load_calls()).mxfp4_quantize(x, codes, scales, gated, n_rows, stream)
     if rc:
         _check(rc, "vp_mxfp4_quantize")
@@ -612,7 +622,7 @@ def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: Optional[to
                      n_rows: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """``vp_mxfp4_dequantize``: the values that codes and scales stand for, in ``out``'s type (default bfloat16)."""
     if out is None:
-        out = torch.empty((codes.shape[0], codes.shape[1] * 2), dtype=torch.bfloat16, device=codes.device)
+        out = _alloc(torch.empty, (codes.shape[0], codes.shape[1] * 2), torch.bfloat16, codes.device, stream)
     rc = (_calls or _load_calls()).mxfp4_dequantize(codes, scales, out, n_rows, stream)
     if rc:
         _check(rc, "vp_mxfp4_dequantize")
@@ -625,9 +635,9 @@ def mxfp4_product(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.
     rows ``expert_off[e] .. expert_off[e + 1]`` with matrix ``e``.  Returns ``(out, status)``: ``[n, F]`` (default bfloat16; rows
     outside the offsets keep what they hold) and int32[1], into which status bits are OR-ed."""
     if out is None:
-        out = torch.empty((x_codes.shape[0], w_codes.shape[1]), dtype=torch.bfloat16, device=x_codes.device)
+        out = _alloc(torch.empty, (x_codes.shape[0], w_codes.shape[1]), torch.bfloat16, x_codes.device, stream)
     if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=x_codes.device)
+        status = _alloc(torch.zeros, 1, torch.int32, x_codes.device, stream)
     rc = (_calls or _load_calls()).mxfp4_product(x_codes, x_scales, w_codes, w_scales, expert_off, out, status, stream)
     if rc:
         _check(rc, "vp_mxfp4_product")
