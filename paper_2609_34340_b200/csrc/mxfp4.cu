@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "elements.cuh"
+#include "row_pieces.h"
 
 namespace {
 
@@ -124,8 +125,8 @@ __device__ __forceinline__ float power_of_two(int e) { return __int_as_float(e >
 struct Piece { int r, c; };
 __device__ __forceinline__ bool piece_of(const MxArgs& a, int r0, int c0, int rows, int u, Piece& p) {
     const int i = c0 + u * kMxThreads + (int)threadIdx.x, down = a.by_groups.div(i);
-    p = Piece{min(r0 + down, rows - 1), i - down * a.groups};
-    return r0 + down < rows;
+    p.c = i - down * a.groups;
+    return row_below(r0, down, rows, p.r);
 }
 
 // N pieces a thread, all loaded before the first is worked on.  GATED: rows are 2 K wide, the value is silu(x[k]) * x[K + k], in 32

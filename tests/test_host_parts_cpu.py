@@ -244,3 +244,21 @@ int main() {
         }
 }
 ''')
+
+
+def test_rows_of_pieces_at_the_largest_row_count(tmp_path):
+    """Rows are below 2^31, and a CTA's last pieces lie up to 256 rows below its first: the row of a piece stays one of the rows in use."""
+    _run(tmp_path, r'''
+#include "row_pieces.h"
+#include <stdint.h>
+int main() {
+    for (int64_t rows : {(int64_t)1, (int64_t)2, (int64_t)100, (int64_t)1 << 30, ((int64_t)1 << 31) - 300, ((int64_t)1 << 31) - 1})
+        for (int64_t first = rows > 600 ? rows - 600 : 0; first < rows; first++)
+            for (int down = 0; down <= 256; down++) {
+                int row = -1;
+                const bool in = row_below((int)first, down, (int)rows, row);
+                assert(in == (first + down < rows));
+                assert(row == (in ? first + down : rows - 1));
+            }
+}
+''')
