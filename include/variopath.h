@@ -590,7 +590,7 @@ int vp_mxfp4_dequantize(const uint8_t* codes, int64_t codes_ld, const uint8_t* s
  *              read nor written.
  *   out        [capacity_rows][out_ld] of `dtype`; may not overlap the inputs
  *   status     int32[1], bits are OR-ed in (not cleared): VP_ST_PACK_MISMATCH if an offset falls or lies outside
- *              0 .. capacity_rows (offsets are then clamped), VP_ST_INTERNAL_TIMEOUT if a bounded wait inside the kernel gave up (out
+ *              0 .. capacity_rows (offsets are then clamped, and a row belongs to the first expert that reaches it), VP_ST_INTERNAL_TIMEOUT if a bounded wait inside the kernel gave up (out
  *              is incomplete)
  * Limits: E <= 1024, K and F <= 2^20, else VP_E_UNSUPPORTED; K a multiple of 32.  capacity_rows also chooses the launch shape (from 192
  * rows per expert on pairs of CTAs): a step with few rows in a large buffer is best given the part of it that it can use.

@@ -157,20 +157,17 @@ __device__ __forceinline__ void load_columns(unsigned tmem, unsigned (&r)[32]) {
         : "r"(tmem) : "memory");
 }
 
-// The experts that have rows, in order: id, and the row tiles in front of them.
+// The experts that have rows, in order: id, first row, and the row tiles in front of them.  No row has two experts, whatever the offsets
+// are, so there are at most a tile per expert more than the rows fill, and their numbers stay within 32 bits.
 struct Experts {
     int* tiles;                                   // one entry more
+    int* first;
     uint16_t* id;
     int n;
 };
 
-// Rows of an expert; offsets are held inside the buffer whatever they are.
-struct Rows { int first, n; };
-__device__ __forceinline__ Rows rows_of(const ProductArgs& a, int e, bool& bad) {
-    const int lo = a.off[e], hi = a.off[e + 1], first = min(max(lo, 0), a.R);
-    bad = lo < 0 || hi < lo || hi > a.R;
-    return Rows{first, max(min(max(hi, 0), a.R) - first, 0)};
-}
+// An offset, held inside the buffer whatever it is.
+__device__ __forceinline__ int offset_of(const ProductArgs& a, int e) { return min(max(a.off[e], 0), a.R); }
 
 struct Tile {
     int e, first, rows, n0;                       // expert, first row, rows (at most mt), first feature
@@ -183,11 +180,9 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a, const Experts& x, 
         const int mid = (lo + hi + 1) / 2;
         if ((long long)x.tiles[mid] * n_tiles <= tile) lo = mid; else hi = mid - 1;
     }
-    bool bad;
-    const Rows r = rows_of(a, x.id[lo], bad);
-    const int m_tiles = x.tiles[lo + 1] - x.tiles[lo];
-    const int q = (int)(tile - (long long)x.tiles[lo] * n_tiles), m = q % m_tiles;
-    return Tile{x.id[lo], r.first + m * mt, min(mt, r.n - m * mt), q / m_tiles * nt};
+    const int e = x.id[lo], m_tiles = x.tiles[lo + 1] - x.tiles[lo];
+    const int q = (int)(tile - (long long)x.tiles[lo] * n_tiles), m = q % m_tiles, first = x.first[lo] + m * mt;
+    return Tile{e, first, min(mt, offset_of(a, e + 1) - first), q / m_tiles * nt};
 }
 
 // 32 scales of a row.
@@ -256,7 +251,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x % CG);          // of the pair
     const unsigned base = (smem_u32(s_raw) + 1023) & ~1023u;
     int* const lists = (int*)(s_raw + (base - smem_u32(s_raw)) + S::lists_begin);
-    Experts ex{lists, (uint16_t*)(lists + a.E + 1), 0};
+    Experts ex{lists, lists + a.E + 1, (uint16_t*)(lists + 2 * a.E + 1), 0};
     const unsigned bars = smem_u32(s_bar);
     const auto first_cta = [&](unsigned bar) { return CG == 1 ? bar : in_cta(bar, 0); };
     const auto full = [&](int s) { return bars + 8 * s; };                                  // of the first CTA: what a stage needs is there
@@ -289,16 +284,23 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     }
     grid_wait();
     if (warp == 0) {                              // experts with rows
-        int n = 0, tiles = 0, most = 0;
+        int n = 0, tiles = 0, most = 0, end = 0;                   // end: the largest offset so far
         bool bad = false;
         for (int e0 = 0; e0 < a.E; e0 += 32) {
             const int e = e0 + lane;
-            int rows = 0;
+            int first = 0, next = 0;
             if (e < a.E) {
-                bool wrong;
-                rows = rows_of(a, e, wrong).n;
-                bad |= wrong;
+                first = offset_of(a, e);
+                next = offset_of(a, e + 1);
+                bad |= a.off[e] != first || a.off[e + 1] != next || next < first;
             }
+            bad = __any_sync(kAll, bad);
+            if (bad) {                            // a row belongs to the first expert that reaches it
+                first = max(first, end);
+                for (int o = 1; o < 32; o *= 2) first = max(first, __shfl_up_sync(kAll, first, o));
+            }
+            end = max(end, __reduce_max_sync(kAll, max(first, next)));
+            const int rows = max(next - first, 0);
             most = max(most, rows);
             int sum = (rows + MT - 1) / MT;
             const int own = sum;
@@ -310,6 +312,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
             if (rows > 0) {
                 const int at = n + __popc(who & ((1u << lane) - 1));
                 ex.id[at] = (uint16_t)e;
+                ex.first[at] = first;
                 ex.tiles[at] = tiles + sum - own;
             }
             n += __popc(who);
@@ -321,7 +324,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
             s_n = n;
             s_most = most;
         }
-        if (bad && blockIdx.x == 0) atomicOr(a.status, VP_ST_PACK_MISMATCH);
+        if (bad && lane == 0 && blockIdx.x == 0) atomicOr(a.status, VP_ST_PACK_MISMATCH);
     }
     fence_before();
     __syncthreads();
@@ -601,7 +604,7 @@ bool make_map(CUtensorMap* map, int rank, const void* p, const cuuint64_t* dims,
 }
 
 template <int CG>
-size_t product_smem(int E) { return (size_t)Shape<CG>::lists_begin + 1024 + (size_t)E * 6 + 4; }
+size_t product_smem(int E) { return (size_t)Shape<CG>::lists_begin + 1024 + (size_t)E * 10 + 4; }
 
 template <int CG, typename T>
 cudaError_t launch_product(const CUtensorMap (&x_maps)[3], const CUtensorMap& w_map, const ProductArgs& a, int grid,

@@ -373,6 +373,37 @@ def test_product_reports_offsets_that_fall_or_leave_the_buffer(vp):
         assert ((got.double() - want).abs()[inside] <= _bound(o, size, want, torch.float32)[inside]).all()
 
 
+def test_product_of_offsets_that_fall_gives_a_row_to_the_first_expert_that_reaches_it(vp):
+    """Ranges that overlap as given: no row has two experts, and no row is summed twice."""
+    o = _operands([50, 50, 30], 160, 320, 17, spare=70)
+    for off, rows in (([0, 100, 50, 120], (100, 0, 20)), ([40, 10, 60, 50], (0, 20, 0)), ([0, 200, 0, 200], (200, 0, 0)), ([-7, 3, -9, 999], (3, 0, 197))):
+        o["off"] = torch.tensor(off, dtype=torch.int32)
+        at = min(max(off[0], 0), 200)
+        want, size, used = torch.zeros(200, 160).double(), torch.zeros(200, 160).double(), torch.zeros(200, dtype=torch.bool)
+        x, w = ref.decode(o["xc"], o["xs"]), ref.decode(o["wc"], o["ws"])
+        for e, n in enumerate(rows):
+            want[at:at + n], size[at:at + n], used[at:at + n] = x[at:at + n] @ w[e].T, x[at:at + n].abs() @ w[e].abs().T, True
+            at += n
+        got, status = _product(vp, o, torch.float32)
+        assert status == vp.ST_PACK_MISMATCH
+        assert ((got.double() - want).abs() <= _bound(o, size, want, torch.float32))[used].all() and (got[~used] == 3).all()
+
+
+def test_product_of_many_experts_whose_offsets_fall(vp):
+    """Offsets that fall again and again over several groups of 32 experts, behind groups whose offsets rise."""
+    E = 100
+    o = _operands([1] * E, 8, 32, 18, spare=28)
+    off = list(range(40)) + [90 if e % 2 else 20 for e in range(40, E + 1)]
+    o["off"] = torch.tensor(off, dtype=torch.int32)
+    x, w = ref.decode(o["xc"], o["xs"]), ref.decode(o["wc"], o["ws"])
+    expert = [e for e in range(39)] + [40] * (90 - 39)                # (expert 39 has none: its end is before its beginning)
+    want = torch.stack([x[r] @ w[e].T for r, e in enumerate(expert)])
+    size = torch.stack([x[r].abs() @ w[e].abs().T for r, e in enumerate(expert)])
+    got, status = _product(vp, o, torch.float32)
+    assert status == vp.ST_PACK_MISMATCH
+    assert ((got[:90].double() - want).abs() <= _bound(o, size, want, torch.float32)).all() and (got[90:] == 3).all()
+
+
 def test_product_in_a_graph_and_on_two_streams(vp):
     o, q = _operands([300, 200], 512, 512, 8), _operands([70, 430], 512, 512, 9)
     dev = {k: (v.cuda() if torch.is_tensor(v) else v) for k, v in o.items()}
