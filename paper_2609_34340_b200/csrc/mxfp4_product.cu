@@ -24,6 +24,7 @@
 #include "bulk_copy.cuh"
 #include "elements.cuh"
 #include "odd_words.h"
+#include "ring_drain.h"
 
 namespace {
 
@@ -34,7 +35,7 @@ constexpr int kPrK = 256;                         // values of k per stage: one 
 constexpr int kPrBox = 32;                        // the least rows of a stage
 constexpr int kPrThreads = 320;
 constexpr int kPrLine = 64;                       // bytes of an output row that leave together
-constexpr unsigned kPrPolls = 1u << 22;
+constexpr unsigned kPrPolls = 1u << 22, kPrDrainPolls = 1u << 16;
 
 // CG: CTAs that share a tile.
 template <int CG>
@@ -66,6 +67,7 @@ struct ProductArgs {
     long long out_ld;
     bool out_wide;                                // rows of the output begin at 16-byte borders
     int32_t* status;
+    unsigned polls;                               // of a wait, at most
 };
 
 // An address of this CTA's shared memory in the CTA of that rank of the cluster.
@@ -86,6 +88,9 @@ __device__ __forceinline__ void cluster_expect_tx(unsigned bar, unsigned bytes) 
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
 }
+// Stores to an address of the cluster's shared memory.
+__device__ __forceinline__ void cluster_store(unsigned at, unsigned x) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory"); }
+__device__ __forceinline__ void cluster_store(unsigned at, unsigned long long x) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(x) : "memory"); }
 // Boxes of a tensor map into this CTA's shared memory (no multicast); the barrier may be the pair's first CTA's.
 template <int CG>
 __device__ __forceinline__ void tma_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
@@ -235,6 +240,25 @@ __device__ __forceinline__ void load_scales(const uint8_t* const (&row)[4], cons
     for (int j = 0; j < 4; j++) v[j] = odd[j];
 }
 
+// A wait has run out: its CTA's flag, and the other's of a pair.  Out of line, as what stands in none of the loops.
+template <int CG>
+__device__ __noinline__ void give_up(unsigned stop, int32_t* status) {
+    for (int i = 0; i < CG; i++) cluster_store(in_cta(stop, i), 1u);
+    atomicOr(status, VP_ST_INTERNAL_TIMEOUT);
+}
+// The end of a call that was given up.  Copies that are still on their way are counted on the first CTA's barriers, whichever CTA asked for
+// them; products that are still running are waited for by the lane that issued them.
+template <int CG>
+__device__ __noinline__ void finish_stopped(const unsigned long long* made, int stages, unsigned full, unsigned drained, int rank, bool issues) {
+    if (threadIdx.x == 0 && rank == 0)
+        drain_ring(made, 2 * CG, CG, stages, [&](int i) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + 8 * i) : "memory"); },
+                   [&](int i, unsigned parity) { mbar_wait_bounded(full + 8 * i, parity, kPrDrainPolls); });
+    if (issues) {
+        if (rank == 0) mma_commit<CG>(drained);
+        mbar_wait_bounded(drained, 0, kPrDrainPolls);
+    }
+}
+
 template <int CG, typename T>
 __global__ void __launch_bounds__(kPrThreads, 1)
 mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap x_64_map,
@@ -246,6 +270,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     __shared__ unsigned s_tmem;
     __shared__ int s_n, s_most;
     __shared__ volatile int s_stop;
+    __shared__ unsigned long long s_made[2 * CG]; // of the first CTA: stages that each CTA's operands were asked for, whose scales it passed on
     static_assert(3 * S::most_stages + 5 <= 64, "a thread per barrier");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x % CG);          // of the pair
@@ -334,16 +359,18 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     const unsigned tmem = s_tmem;
     const int n_tiles = (a.F + NT - 1) / NT, k_tiles = (a.K + kPrK - 1) / kPrK;
     const long long tiles = (long long)ex.tiles[ex.n] * n_tiles, t0 = blockIdx.x / CG, step = gridDim.x / CG;
-    // Every wait is bounded: the one that gives up sets the flag, which ends the others' (of the other CTA by their own limits).
+    // Every wait is bounded: the one that gives up sets the flag, which ends the others', in both CTAs.  (The count is looked at behind a poll: in
+    // front of it, one row of 7,168 x 4,096 took 11.6 us instead of 11.0.)
     const auto wait = [&](unsigned bar, unsigned parity) {
-        for (unsigned i = 0; i < kPrPolls; i++) {
+        unsigned i = 0;
+        do {
             if (mbar_try_wait(bar, parity)) return true;
             if (s_stop) return false;
-        }
-        s_stop = 1;
-        atomicOr(a.status, VP_ST_INTERNAL_TIMEOUT);
+        } while (++i < a.polls);
+        give_up<CG>(smem_u32((const void*)&s_stop), a.status);
         return false;
     };
+    const auto made = [&](int i, unsigned long long stages) { cluster_store(first_cta(smem_u32(&s_made[i])), stages); };
     // One CTA: where no expert has more than 32 or 64 rows, a stage holds that many, and there are more stages (the products read 128 rows
     // all the same: what lies behind, any bits being numbers, makes rows that nobody stores).  They come as one box, whosever they are:
     // four boxes of 32 cost as much time as their bytes (16,384 rows, 7,168 x 4,096: 212 us against 175), which is also why tiles do not
@@ -359,9 +386,11 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     const auto stage_at = [&](int st) { return base + st * (a_bytes + S::b_bytes + S::s_bytes); };
     const auto scales_at = [&](int st) { return stage_at(st) + a_bytes + S::b_bytes; };
 
+    bool one = false;                             // the lane of warp 1 that issues
     if (warp == 0) {
         if (lane == 0) {
             bool ok = true;
+            unsigned long long asked = 0;
             for (long long t = t0; ok && t < tiles; t += step) {
                 const Tile tile = tile_of(a, ex, t, n_tiles, MT, NT);
                 const CUtensorMap* const map = a_rows == kPrM ? &x_map : (a_rows == kPrBox ? &x_32_map : &x_64_map);
@@ -374,6 +403,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
                     tma_3d<CG>(at + a_bytes, &w_map, k * (kPrK / 2), tile.n0 + rank * 128, tile.e, bar);
                     tma_2d<CG>(at, map, k * (kPrK / 2), tile.first + rank * kPrM, bar);
                     s.next(stages);
+                    asked++;
                 }
             }
             // The pair's first CTA arrives at this one's barriers until the last stage has been read.
@@ -381,10 +411,10 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
                 ok = wait(empty(s.at), s.phase ^ 1);
                 s.next(stages);
             }
-            if (!ok)                              // copies that are still on their way (bounded as well)
-                for (int i = 0; i < stages; i++) mbar_wait_bounded(full(i), i < s.at ? s.phase : s.phase ^ 1, 1u << 16);
+            made(rank, asked);
         }
     } else if (warp == 1) {
+        one = elect_one();
         // The whole warp goes along, so that what the instructions take is the same in all lanes and known to be; one lane issues them.
         if (rank == 0) {
             const unsigned tm = __reduce_max_sync(kAll, tmem), rows_bytes = __reduce_max_sync(kAll, (unsigned)a_bytes),
@@ -392,7 +422,6 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
                            stage16 = (rows_bytes + S::b_bytes + S::s_bytes) >> 4;
             constexpr unsigned idesc = 1u << 7 | 1u << 10 | (unsigned)(NT >> 3) << 17 | 1u << 23 | (unsigned)(MT >> 7) << 27;
             const int my_tiles = __reduce_max_sync(kAll, t0 < tiles ? (int)((tiles - 1 - t0) / step) + 1 : 0);
-            const bool one = elect_one();
             bool ok = true;
             unsigned st = 0, parity = 0;
             for (int j = 0; ok && j < my_tiles; j++) {
@@ -422,10 +451,6 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
                 }
                 if (ok && one) mma_commit<CG>(done(j & 1));
                 __syncwarp();
-            }
-            if (!ok && one) {                     // products that are still running
-                mma_commit<CG>(drained);
-                mbar_wait_bounded(drained, 0, 1u << 16);
             }
         }
     } else if (warp < 4 || (warp == 8 && CG == 2)) {
@@ -479,6 +504,7 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
         // wait in the warps that load.  (What it fences has been seen by its wait; the arrival behind it is what the copies wait for.)
         if (lane == 0) {
             bool ok = true;
+            unsigned long long passed = 0;
             for (long long t = t0; ok && t < tiles; t += step)
                 for (int k = 0; k < k_tiles; k++) {
                     if (!(ok = wait(written(s.at), s.phase))) break;
@@ -486,7 +512,9 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
                     if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full(s.at)) : "memory");
                     else cluster_arrive(first_cta(full(s.at)));
                     s.next(stages);
+                    passed++;
                 }
+            made(CG + rank, passed);
         }
     } else if (warp < 8) {
         const int quarter = warp - 4;             // lanes 32 * quarter .. of tensor memory: rows of the tile
@@ -569,6 +597,11 @@ mxfp4_product_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_con
     __syncwarp();
     __syncthreads();
     if constexpr (CG > 1) cluster_sync();         // (nobody leaves while its memory is read or its barriers are arrived at)
+    if (s_stop) {                                 // (in both CTAs or in none, and nobody begins anything any more)
+        finish_stopped<CG>(s_made, stages, full(0), drained, rank, one);
+        __syncthreads();
+        if constexpr (CG > 1) cluster_sync();
+    }
     if (warp == 1) {
         fence_after();
         if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
@@ -633,6 +666,14 @@ cudaError_t launch_product(const CUtensorMap (&x_maps)[3], const CUtensorMap& w_
 extern "C" int vp_mxfp4_product(const uint8_t* x_codes, int64_t x_codes_ld, const uint8_t* x_scales, int64_t x_scales_ld,
                                 int64_t capacity_rows, const uint8_t* w_codes, const uint8_t* w_scales, int E, int64_t F, int64_t K,
                                 const int32_t* expert_off, void* out, int dtype, int64_t out_ld, int32_t* status, void* cuda_stream) {
+    return vp_mxfp4_product_polls(x_codes, x_codes_ld, x_scales, x_scales_ld, capacity_rows, w_codes, w_scales, E, F, K, expert_off, out, dtype, out_ld,
+                                  status, cuda_stream, kPrPolls);
+}
+
+extern "C" int vp_mxfp4_product_polls(const uint8_t* x_codes, int64_t x_codes_ld, const uint8_t* x_scales, int64_t x_scales_ld,
+                                      int64_t capacity_rows, const uint8_t* w_codes, const uint8_t* w_scales, int E, int64_t F, int64_t K,
+                                      const int32_t* expert_off, void* out, int dtype, int64_t out_ld, int32_t* status, void* cuda_stream,
+                                      unsigned polls) {
     if (!is_type(dtype) || capacity_rows < 0 || E <= 0 || F <= 0 || K <= 0 || K % VP_MXFP4_BLOCK || out_ld < F || x_codes_ld < K / 2 ||
         x_scales_ld < K / VP_MXFP4_BLOCK || x_codes_ld % 16)
         return VP_E_BAD_ARG;
@@ -646,7 +687,7 @@ extern "C" int vp_mxfp4_product(const uint8_t* x_codes, int64_t x_codes_ld, cons
     const int sms = sm_count_of_device();
     if (!sms) return VP_E_CUDA;
     const ProductArgs a{x_scales, w_scales, x_scales_ld, expert_off, E, (int)capacity_rows, (int)F, (int)K, out, out_ld,
-                        (uintptr_t)out % 16 == 0 && out_ld * size % 16 == 0, status};
+                        (uintptr_t)out % 16 == 0 && out_ld * size % 16 == 0, status, polls};
     // Row tiles there can be at most: a part of one per expert more than the rows fill.
     const auto most_tiles = [&](int mt, int nt) { return ((capacity_rows + mt - 1) / mt + (E < capacity_rows ? E : capacity_rows)) * ((F + nt - 1) / nt); };
     // A pair where experts have rows for 256 (16 x 128 rows, half of a pair's rows empty: 65 us against 57 of one CTA; 8 x 384 63 against 80) and

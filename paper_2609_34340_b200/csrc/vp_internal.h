@@ -135,6 +135,12 @@ int vp_schedule_launch(const vp_catalog* c, const vp_sched_params* p, const int6
                        int64_t* send_off, int64_t* recv_off, int64_t* tau_ns_out, int32_t* status, void* workspace,
                        size_t workspace_bytes, void* cuda_stream, bool host_rows);
 
+// vp_mxfp4_product whose waits give up after that many polls (for tests of what happens then).
+extern "C" int vp_mxfp4_product_polls(const uint8_t* x_codes, int64_t x_codes_ld, const uint8_t* x_scales, int64_t x_scales_ld,
+                                      int64_t capacity_rows, const uint8_t* w_codes, const uint8_t* w_scales, int E, int64_t F, int64_t K,
+                                      const int32_t* expert_off, void* out, int dtype, int64_t out_ld, int32_t* status, void* cuda_stream,
+                                      unsigned polls);
+
 extern std::atomic<long long> g_vp_launches;
 
 // Profiling hook: when enabled, records a CUDA event on `stream` before (edge 0) / after (edge 1)

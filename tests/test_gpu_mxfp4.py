@@ -1,4 +1,5 @@
 """GPU tests of vp_mxfp4_quantize, vp_mxfp4_dequantize and vp_mxfp4_product against the definitions in 64 bits."""
+import ctypes
 import math
 import os
 
@@ -430,6 +431,32 @@ def test_product_in_a_graph_and_on_two_streams(vp):
             call(to, s)
     torch.cuda.synchronize()
     assert torch.equal(outs[0], out) and torch.equal(outs[1], out) and int(status) == 0
+
+
+@pytest.mark.parametrize("counts,F,K", [([1], 520, 7168), ([60, 20, 3], 600, 1056), ([2100], 2304, 2080), ([3000, 500], 4096, 1024)])
+def test_product_whose_waits_run_out_reports_it_and_leaves_the_device_as_it_was(vp, counts, F, K):
+    """Waits of few polls: the call ends, the status says so, rows outside the offsets keep what they hold, and the next call is right."""
+    o = _operands(counts, F, K, F, spare=9)
+    want, size = _expected(o)
+    codes, scales = _wire(vp, o)
+    wc, ws, off = o["wc"].cuda(), o["ws"].cuda(), o["off"].cuda()
+    n, gave_up = sum(counts), 0
+    fn = vp.binding._load().vp_mxfp4_product_polls
+    for polls in (0, 1, 2, 3, 5, 8, 20, 60, 200, 1000, 1 << 22):
+        out = torch.full((o["cap"], F), 3.0, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        i64, P = ctypes.c_int64, ctypes.c_void_p
+        rc = fn(P(codes.data_ptr()), i64(codes.stride(0)), P(scales.data_ptr()), i64(scales.stride(0)), i64(o["cap"]), P(wc.data_ptr()), P(ws.data_ptr()),
+                len(counts), i64(F), i64(K), P(off.data_ptr()), P(out.data_ptr()), 2, i64(F), P(status.data_ptr()),
+                P(torch.cuda.current_stream().cuda_stream), ctypes.c_uint(polls))
+        assert rc == 0
+        torch.cuda.synchronize()
+        assert int(status) in (0, vp.ST_INTERNAL_TIMEOUT) and (out[n:] == 3).all()
+        if int(status) == 0:
+            assert ((out.cpu().double() - want).abs() <= _bound(o, size, want, torch.float32))[:n].all()
+        gave_up += int(status) != 0
+        _check(vp, o, torch.float32)
+    assert gave_up > 0 and int(status) == 0
 
 
 def test_product_refuses(vp):

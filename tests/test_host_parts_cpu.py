@@ -262,3 +262,76 @@ int main() {
             }
 }
 ''')
+
+
+def test_a_ring_that_is_given_up_waits_for_every_byte(tmp_path):
+    """One or two CTAs' loaders ask for a stage's bytes and warps pass its scales on, in any order and with any lead that the ring allows, and
+    stop anywhere while any part of the bytes is on its way.  The end of the ring makes each lacking arrival once, none too many, and every
+    byte has come when its last wait returns."""
+    _run(tmp_path, r'''
+#include "ring_drain.h"
+#include <deque>
+#include <random>
+#include <vector>
+struct Barrier {                         // phases in order; a phase ends when nothing is pending
+    int count, pending;
+    long long bytes = 0;
+    unsigned long long phase = 0;
+    explicit Barrier(int n) : count(n), pending(n) {}
+    void ends() { if (pending == 0 && bytes == 0) { phase++; pending = count; } }
+    void arrive() { assert(pending > 0); pending--; ends(); }
+    bool passed(unsigned parity) const { return (phase & 1) != parity; }
+};
+int main() {
+    std::mt19937 rng(1);
+    const auto below = [&](int n) { return (int)(rng() % n); };
+    int unfinished = 0;
+    for (int trial = 0; trial < 200000; trial++) {
+        const int loaders = 1 + below(2), makers = 2 * loaders, stages = 1 + below(9), total = below(30);
+        std::vector<Barrier> full(stages, Barrier(makers));
+        std::vector<unsigned long long> made(makers, 0);
+        std::deque<std::pair<int, int>> flight;          // barrier, bytes
+        unsigned long long used = 0;                     // stages that have been read
+        for (int step = below(200); step; step--) {
+            const int who = below(makers + 2);
+            if (who < makers) {
+                const unsigned long long q = made[who];
+                if (q >= (unsigned long long)total || q >= used + stages) continue;       // (its wait for an empty stage)
+                Barrier& b = full[q % stages];
+                assert(b.phase == q / stages);
+                if (who < loaders) {
+                    b.bytes += 10;
+                    flight.push_back({(int)(q % stages), 4});
+                    flight.push_back({(int)(q % stages), 6});
+                }
+                b.arrive();
+                made[who]++;
+            } else if (who == makers) {
+                if (flight.empty()) continue;
+                const int i = below((int)flight.size());
+                const auto f = flight[i];
+                flight.erase(flight.begin() + i);
+                full[f.first].bytes -= f.second;
+                full[f.first].ends();
+            } else if (used < (unsigned long long)total && full[used % stages].phase > used / stages) {
+                used++;
+            }
+        }
+        unfinished += !flight.empty();
+        drain_ring(made.data(), makers, loaders, stages, [&](int at) { full[at].arrive(); }, [&](int at, unsigned parity) {
+            for (auto f = flight.begin(); f != flight.end();)            // what is on its way to this barrier comes
+                if (f->first == at) {
+                    full[at].bytes -= f->second;
+                    full[at].ends();
+                    f = flight.erase(f);
+                } else {
+                    ++f;
+                }
+            assert(full[at].passed(parity));
+        });
+        assert(flight.empty());
+        for (const Barrier& b : full) assert(b.bytes == 0);
+    }
+    assert(unfinished > 1000);
+}
+''')
