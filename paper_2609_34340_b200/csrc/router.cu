@@ -568,7 +568,7 @@ extern "C" int vp_route(const vp_route_params* p, const void* logits, int dtype,
     a.wide_bias = bias && (uintptr_t)bias % 16 == 0;
     a.n_group = p->n_group; a.topk_group = p->topk_group; a.group_top = p->group_top; a.per = p->experts / p->n_group;
     a.scale = p->scale; a.idx = expert_idx; a.weights = weights;
-    const int warps = route_warps(T, sms), grid = (T + warps - 1) / warps;
+    const int warps = route_warps(T, sms), grid = (int)(((long long)T + warps - 1) / warps);
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
@@ -602,7 +602,7 @@ extern "C" int vp_route_backward(const vp_route_params* p, const void* logits, i
     a.sigmoid = p->scoring == VP_SCORE_SIGMOID; a.renormalise = p->renormalise != 0; a.wide = rows_aligned(logits, ld, size, 16);
     a.scale = p->scale; a.idx = expert_idx; a.grad = grad_weights; a.out = grad_logits; a.out_ld = grad_ld;
     a.out_wide = rows_aligned(grad_logits, grad_ld, size, 16) && a.E * size % 16 == 0;
-    const int warps = route_warps(T, sms), grid = (T + warps - 1) / warps;
+    const int warps = route_warps(T, sms), grid = (int)(((long long)T + warps - 1) / warps);
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;

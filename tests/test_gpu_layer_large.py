@@ -40,6 +40,21 @@ def test_route_of_many_tokens(vp):
     assert ((out[rows].cpu().double() - slope).abs() <= 1e-5 * size + 2.0 ** -8 * slope.abs() + 1e-37).all()
 
 
+def test_route_of_as_many_tokens_as_there_may_be(vp):
+    """One expert, 2^31 - 1 tokens: the launch's size is worked out without leaving 32 bits."""
+    T = (1 << 31) - 1
+    p = vp.RouteParams(1, 1, "sigmoid", 1, 1, 1, False, 1.0)
+    z = torch.zeros(T, 1, device="cuda", dtype=torch.bfloat16)
+    z[-2:] = 1.0
+    idx, w = vp.route(p, z)
+    s = 1 / (1 + torch.exp(torch.tensor(-1.0, dtype=torch.float64)))
+    assert int(idx.view(-1)[::4097].abs().sum()) == 0 and (idx[-5:] == 0).all()
+    assert torch.allclose(w[-5:].view(-1).cpu().double(), torch.tensor([0.5] * 3 + [float(s)] * 2, dtype=torch.float64), rtol=1e-6)
+    out = vp.route_backward(p, z, idx, w.fill_(1.0))
+    want = torch.tensor([0.25] * 3 + [float(s * (1 - s))] * 2, dtype=torch.float64)
+    assert torch.allclose(out[-5:].view(-1).cpu().double(), want, rtol=2.0 ** -8)
+
+
 def test_combine_of_many_rows(vp):
     T, topk, H = 4099, 64, 8200
     assert T * topk * H > 1 << 31
