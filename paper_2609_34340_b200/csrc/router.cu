@@ -17,6 +17,7 @@
 #include <type_traits>
 
 #include "elements.cuh"
+#include "route_bound.h"
 
 namespace {
 
@@ -273,10 +274,7 @@ route_kernel(const __grid_constant__ RouteArgs a) {
                 if (by[v] > -CUDART_INF_F) largest = fmaxf(largest, fabsf(by[v]));
             largest = warp_max(largest);
         }
-        // Twice a bound of a key's error, in units of 2^-24.  Sigmoid: d s = s (1 - s) d(exp) / exp, with |z| + 4 for the exponential, 3 for the
-        // quotient's two steps: below 5.  Softmax: of the largest score, |z - max| s (at most 1/e) + 4 for an exponential, the same and VPL + 5
-        // additions for their sum, 2 for its reciprocal: below VPL + 20.  The sum with the bias: half a unit of the key.
-        tol = over * (a.sigmoid ? 2e-6f : (VPL + 20) * 1.2e-7f) + 2.5e-7f * largest;
+        tol = over * twice_score_error(a.sigmoid, VPL) + 2.5e-7f * largest;       // (the sum with the bias: half a unit of the key)
     }
     if (a.n_group > 1) {
         float mine = -CUDART_INF_F;

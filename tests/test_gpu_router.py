@@ -155,6 +155,24 @@ def test_route_chooses_as_64_bits_do(vp, scoring, n_group, topk_group, group_top
     _check(vp, p, torch.cat([z, near]), bias)
 
 
+@pytest.mark.parametrize("experts", [64, 256, 1000, 1024])
+@pytest.mark.parametrize("apart", [3e-7, 1e-6, 4e-6, 1.2e-5])
+def test_route_chooses_as_64_bits_do_where_the_softmax_sum_is_least_certain(vp, experts, apart):
+    """One logit ahead and all others equally far behind, where the sum of the exponentials is off by most; biases that leave keys a step of
+    about the error's bound apart, in a random order."""
+    g = _gen(experts)
+    p = vp.RouteParams(experts, 8, "softmax", 1, 1, 1, True, 1.0)
+    far = 4.0
+    for _ in range(50):                               # the distance at which the mean distance under the softmax, far - 1, is largest
+        far = math.log((experts - 1) / (far - 1))
+    z = torch.full((1, experts), -far) + torch.rand(1, experts, generator=g) * 1e-3
+    z[0, experts // 3] = 0.0
+    _, s, _ = ref.scores(p, z)
+    bias = (0.5 - s[0] + torch.randperm(experts, generator=g).double() * apart / 4).to(torch.float32)
+    near = z + torch.randn(40, experts, generator=g) * 1e-6
+    _check(vp, p, torch.cat([z, near]), bias)
+
+
 def test_route_of_strided_and_unaligned_logits(vp):
     g = _gen(5)
     p = vp.RouteParams(96, 6, "sigmoid", 4, 2, 2, True, 1.0)

@@ -335,3 +335,32 @@ int main() {
     assert(unfinished > 1000);
 }
 ''')
+
+
+def test_bound_of_a_routers_scores(tmp_path):
+    """Counted step by step in units of 2^-24, at the logits where each is largest.  An exponential of -d: the argument's difference, its
+    product with log2 e and that constant's own rounding (0.23 units) make d units each, the function 4 (2^-22).  Softmax: the sum's error is
+    the mean of that under the softmax (largest with all others equally far), an addition per value of a lane and five across lanes; the reciprocal 2, the
+    product 1.  Sigmoid: the exponential without a difference, damped by s (1 - s); the sum 1, the reciprocal 2."""
+    _run(tmp_path, r'''
+#include <cmath>
+#include "route_bound.h"
+int main() {
+    const double u = std::ldexp(1.0, -24);
+    for (int per : {1, 2, 3, 4, 5, 6, 8, 12, 16, 24, 32}) {
+        const int E = 32 * per;
+        double mean = 0, worst = 0;
+        for (double x = 0; x < 40; x += 1e-3) mean = std::fmax(mean, x * (E - 1) * std::exp(-x) / (1 + (E - 1) * std::exp(-x)));
+        for (double d = 0; d < 40; d += 1e-2)
+            worst = std::fmax(worst, std::exp(-d) * (2.23 * d + 4 + (2.23 * mean + 4 + per + 5) + 2 + 1));
+        assert(twice_score_error(false, per) >= 2 * worst * u);
+        assert(twice_score_error(false, per) <= 4 * worst * u);          // (a wide one sends more tokens to the comparison in 64 bits)
+    }
+    double worst = 0;
+    for (double z = -40; z < 40; z += 1e-2) {
+        const double s = 1 / (1 + std::exp(-z));
+        worst = std::fmax(worst, s * (1 - s) * (1.23 * std::fabs(z) + 4) + s * (1 + 2));
+    }
+    assert(twice_score_error(true, 8) >= 2 * worst * u);
+}
+''')
