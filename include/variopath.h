@@ -491,7 +491,7 @@ int vp_unpack_tokens(const int32_t* n_steps_b, const int16_t* lane_dst_b, const 
  * way, the experts' products on what vp_unpack writes, and the weighted sum of what vp_unpack_tokens writes.  All of them
  * enqueue one kernel on cuda_stream of the current device, need no workspace, and wait for nothing; pointers are device
  * pointers, strides (ld) are in elements, zero tokens or rows are accepted and launch nothing.  Results do not depend on the
- * launch geometry: sums have a fixed order.
+ * launch geometry, nor on how many tokens or rows a call has: sums have a fixed order.
  */
 
 /* Element types. */
@@ -548,8 +548,9 @@ int vp_combine(const void* rows, int dtype, const int32_t* expert_idx, const flo
 
 /*
  * vp_combine_backward - grad_rows[t * topk + s] = weights[t][s] * grad[t] (0 for dropped copies: what vp_pack sends back) and
- * grad_weights[t][s] = <grad[t], rows[t * topk + s]> (0 for dropped copies).  Either output may be NULL, rows too when
- * grad_weights is.  No output may overlap an input.  The gradient of base is grad itself.
+ * grad_weights[t][s] = <grad[t], rows[t * topk + s]> (0 for dropped copies, whatever grad[t] holds).  Either output may be
+ * NULL, rows too when grad_weights is.  No output may overlap an input.  The gradient of base is grad itself.  The products of grad_weights are added
+ * up in an order that depends on H, and on whether grad, rows and grad_rows all begin their rows on 16-byte borders.
  */
 int vp_combine_backward(const void* grad, const void* rows, int dtype, const int32_t* expert_idx, const float* weights, int T,
                         int topk, int64_t H, void* grad_rows, float* grad_weights, void* cuda_stream);

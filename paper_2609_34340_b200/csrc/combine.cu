@@ -17,6 +17,7 @@ constexpr int kCombineThreads = 256;
 constexpr int kSlots = 8;                         // slots whose rows are in flight together, at most
 constexpr int kGradThreads = 64, kGradAhead = 5;   // (three to six stages, two or four warps: within 3 %)
 constexpr int kGradShared = 256;
+constexpr int kGradLong = 2 * kGradShared;        // vectors of a row
 constexpr int kCombineMaxTop = 4096;              // (8 bytes of shared memory per slot)
 
 // A vector of a row that is there, zeros for one that is not (its memory may hold anything): loads under a predicate, no branch
@@ -115,8 +116,11 @@ __device__ __forceinline__ void copy_16(unsigned to, const void* from, bool here
 // that nothing waits for another thread and the loads in flight cost no registers: with loads into registers, one step at a time or two,
 // reads and writes together reached 4.9 to 6.1 TB/s (8,192 tokens x 8 of 4,096 bf16 186 to 235 us); so 168 us, 6.8 TB/s.
 // SHARED: the CTA's warps share a token and S slots (with few tokens a call would wait for one warp's steps one after another: a token of
-// 7,168 values, 28 steps, 16.7 us, so 4.6); their sums meet in a fixed order.
-template <typename T, int S, bool SHARED>
+// 7,168 values, 28 steps, 16.7 us, so 4.6).
+// The order of the additions depends on the row's length alone, not on which form a call of so many tokens takes.  Rows of kGradLong vectors
+// and more (LONG) are always SHARED: a thread adds up vectors 256 apart.  Below, vectors are summed by themselves and then added up 32 apart,
+// which a SHARED CTA, with every vector's sum in some thread, does through shared memory.
+template <typename T, int S, bool SHARED, bool LONG>
 __global__ void __launch_bounds__(SHARED ? kGradShared : kGradThreads)
 combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
     constexpr int V = 16 / (int)sizeof(T), kGradStages = SHARED ? 2 : kGradAhead;
@@ -144,11 +148,11 @@ combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
         for (int s = 0; s < S; s++) copy_16(to + (s + 1) * 512, rows + s * n + i, i < n && (read >> s & 1));
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    float w[S], dot[S];
+    float w[S], dot[S], first_dot[S];                // first_dot: a SHARED thread's first vector
 #pragma unroll
     for (int s = 0; s < S; s++) {
         w[s] = __shfl_sync(kAll, own, s);
-        dot[s] = 0;
+        dot[s] = first_dot[s] = 0;
     }
     constexpr int step = SHARED ? kGradShared : 32;
 #pragma unroll
@@ -164,8 +168,12 @@ combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
 #pragma unroll
         for (int s = 0; s < S; s++) {
             const Pack<T, V> x = *(const Pack<T, V>*)(from + (s + 1) * 32);
+            float sum = LONG ? dot[s] : 0;
 #pragma unroll
-            for (int u = 0; u < V; u++) dot[s] = fmaf(f[u], value_of(x.v[u]), dot[s]);
+            for (int u = 0; u < V; u++) sum = fmaf(f[u], value_of(x.v[u]), sum);
+            if (LONG) dot[s] = sum;
+            else if (SHARED && i == first_vector) first_dot[s] = sum;
+            else dot[s] += sum;
         }
         const int last = k == 0 ? kGradStages - 1 : k - 1;
         issue(i + step * (kGradStages - 1), last);
@@ -182,6 +190,25 @@ combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (!a.grad_weights) return;
+    if (SHARED && !LONG) {                        // at most two vectors a thread: their sums side by side, a warp for a slot's
+        float* const sums = (float*)s_stage;
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < S; s++) {
+            sums[s * kGradLong + threadIdx.x] = first_dot[s];
+            sums[s * kGradLong + kGradShared + threadIdx.x] = dot[s];
+        }
+        __syncthreads();
+        if (warp >= slots) return;
+        float part[kGradLong / 32], d = 0;        // (0 behind the row's end)
+#pragma unroll
+        for (int i = 0; i < kGradLong / 32; i++) part[i] = sums[warp * kGradLong + 32 * i + lane];
+#pragma unroll
+        for (int i = 0; i < kGradLong / 32; i++) d += part[i];
+        d = warp_sum(d);
+        if (lane == 0) a.grad_weights[first + warp] = here >> warp & 1 ? d : 0.f;
+        return;
+    }
     float mine = 0;
 #pragma unroll
     for (int s = 0; s < S; s++) {
@@ -305,8 +332,9 @@ extern "C" int vp_combine_backward(const void* grad, const void* rows, int dtype
             };
             // Warps share a token where rows are long or tokens few: 4,096 x 8 of 7,168 bf16 150 against 160 us, 128 x 8 of 1,024 2.5 against
             // 4.0; 1,531 x 6 of 2,048 14.1 against 9.7.
-            if (n >= 512 || (items <= 4 * sms && n > 64)) go(combine_backward_kernel<X, s, true>, (int)items, kGradShared, 2);
-            else go(combine_backward_kernel<X, s, false>, ctas(items), kGradThreads, kGradAhead);
+            if (n >= kGradLong) go(combine_backward_kernel<X, s, true, true>, (int)items, kGradShared, 2);
+            else if (items <= 4 * sms && n > 64) go(combine_backward_kernel<X, s, true, false>, (int)items, kGradShared, 2);
+            else go(combine_backward_kernel<X, s, false, false>, ctas(items), kGradThreads, kGradAhead);
         });
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;

@@ -113,6 +113,22 @@ def test_combine_backward_matches_differences(vp, dtype):
                 assert abs(slope - float(grad_rows[t * topk + s, h])) <= 1.01 * ref.HALF_STEP[dtype] * abs(slope) + 1e-6
 
 
+@pytest.mark.parametrize("topk", [1, 2, 3, 6, 8, 11])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_do_not_depend_on_how_many_tokens_a_call_has(vp, topk, dtype):
+    """The same tokens in a small batch and in a large one: the same bytes, whatever the row length."""
+    for H in (64, 264, 520, 1032, 2048, 4088, 4096, 4104):
+        g = torch.Generator(device="cuda").manual_seed(H + topk)
+        T = 1300
+        rows, grad = (torch.randn(n, H, device="cuda", generator=g).to(dtype) for n in (T * topk, T))
+        idx = torch.randint(-1, 20, (T, topk), device="cuda", dtype=torch.int32, generator=g)
+        w = torch.randn(T, topk, device="cuda", generator=g)
+        large = vp.combine_backward(grad, rows, idx, w)
+        for n in (1, 7, 300):
+            small = vp.combine_backward(grad[:n], rows[:n * topk], idx[:n], w[:n])
+            assert torch.equal(small[0], large[0][:n * topk]) and torch.equal(small[1], large[1][:n]), (H, n)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_combine_of_unaligned_buffers_and_in_place(vp, dtype):
     T, topk, H = 6, 3, 64

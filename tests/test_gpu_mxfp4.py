@@ -299,6 +299,16 @@ def test_product_of_many_tiles(vp, counts, F, K, dtype):
     _check(vp, _operands(counts, F, K, F + K, spare=5), dtype)
 
 
+def test_product_does_not_depend_on_the_launch_shape(vp):
+    """The same rows in a buffer of their own (one CTA to a tile) and in a large one (pairs of CTAs): the same bytes."""
+    for F, K in ((2304, 768), (4096, 2080), (2048, 7168)):
+        o = _operands([100], F, K, F + K, spare=3900)
+        large, status = _product(vp, o, torch.float32)
+        o["cap"], o["xc"], o["xs"] = 100, o["xc"][:100], o["xs"][:100]
+        small, other = _product(vp, o, torch.float32)
+        assert status == other == 0 and torch.equal(large[:100], small)
+
+
 def test_product_of_long_rows(vp):
     _check(vp, _operands([5, 40], 300, 7168, 1), torch.bfloat16)
 
