@@ -11,8 +11,9 @@
 // than twice that bound and do not come from equal logits and biases, those are compared in 64 bits (one token in some 400).
 //
 // Bound by instructions: about 760 a token of 256 experts, of which a quarter are the scores.  16,384 tokens x 256 fp32 logits, sigmoid, bias, best
-// 8 of 4 of 8 groups: 16.0 us (41 with all keys of an unclear token in 64 bits and one expert chosen per round), where reading the
-// logits takes 2.7; 128 tokens 3.4 us, a launch and one warp's chain.
+// 8 of 4 of 8 groups: 16 to 18 us from one run to another (41 with all keys of an unclear token in 64 bits and one expert chosen per round), where
+// reading the logits takes 2.7; 128 tokens 2.9 us, a launch and one warp's chain.  Equal logits leave more than 32 candidates, chosen one by one in
+// 64 bits: the same tokens 78 us then, and 33 without groups and bias.
 #include <cmath>
 #include <type_traits>
 
@@ -232,7 +233,7 @@ route_kernel(const __grid_constant__ RouteArgs a) {
     __shared__ int s_at[kRouteWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = lane * VPL;
     grid_wait();
-    const int t = (int)(blockIdx.x * (blockDim.x >> 5)) + warp;
+    const int t = (int)(blockIdx.x * kRouteWarps) + warp;
     if ((unsigned)t >= (unsigned)a.T) return;     // (the last CTA's warps may pass 2^31)
     const T* const row = (const T*)a.logits + t * a.ld;
     float z[VPL], key[VPL];
@@ -449,14 +450,14 @@ struct RouteGradArgs {
 //   sigmoid               dz_j = g_j s_j (1 - s_j)                    the chosen
 //   sigmoid, renormalised dz_j = w_j (1 - s_j) (g_j - sum_k g_k w_k)  the chosen
 // A warp per token; the row is put together in shared memory and leaves by vectors.  16,384 tokens x 128 bf16 logits, softmax as it is: 6.3 us (its
-// bytes 1.5), bound by instructions and two trips to memory.
+// bytes 1.5), bound by instructions and three trips to memory: indices, the logits at them, the row.
 template <typename T, int VPL>
 __global__ void __launch_bounds__(kRouteWarps * 32)
 route_backward_kernel(const __grid_constant__ RouteGradArgs a) {
     extern __shared__ float s_rows[];             // [warps][E]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = lane * VPL;
     grid_wait();
-    const long long t = (long long)blockIdx.x * (blockDim.x >> 5) + warp;
+    const long long t = (long long)blockIdx.x * kRouteWarps + warp;
     if (t >= a.T) return;
     const T* const row = (const T*)a.logits + t * a.ld;
     float* const out = s_rows + warp * (32 * VPL);
@@ -543,8 +544,8 @@ bool rows_aligned(const void* p, long long ld, int size, int bytes) {
     return (uintptr_t)p % bytes == 0 && (unsigned long long)ld * size % bytes == 0;
 }
 
-// A warp per CTA until every SM has work, four beyond: of 128 tokens every one then has an SM nearly to itself.
-int route_warps(int T, int sms) { return T <= 2 * sms ? 1 : kRouteWarps; }
+// CTAs of kRouteWarps tokens at every size (a warp per CTA instead: 128 tokens 3.1 us against 2.9, 592 3.95 against 4.1, 2,000 4.5 against 4.6).
+int route_ctas(int T) { return (int)(((long long)T + kRouteWarps - 1) / kRouteWarps); }
 
 }  // namespace
 
@@ -558,15 +559,12 @@ extern "C" int vp_route(const vp_route_params* p, const void* logits, int dtype,
     if (!logits || !expert_idx || !weights) return VP_E_BAD_ARG;
     const int size = size_of_type(dtype);
     if ((uintptr_t)logits % size || ((uintptr_t)expert_idx | (uintptr_t)weights | (uintptr_t)bias) % 4) return VP_E_BAD_ARG;
-    const int sms = sm_count_of_device();
-    if (!sms) return VP_E_CUDA;
     RouteArgs a;
     a.logits = logits; a.ld = ld; a.T = T; a.E = p->experts; a.topk = p->topk; a.bias = bias;
     a.sigmoid = p->scoring == VP_SCORE_SIGMOID; a.renormalise = p->renormalise != 0; a.wide = rows_aligned(logits, ld, size, 16);
     a.wide_bias = bias && (uintptr_t)bias % 16 == 0;
     a.n_group = p->n_group; a.topk_group = p->topk_group; a.group_top = p->group_top; a.per = p->experts / p->n_group;
     a.scale = p->scale; a.idx = expert_idx; a.weights = weights;
-    const int warps = route_warps(T, sms), grid = (int)(((long long)T + warps - 1) / warps);
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
@@ -576,8 +574,8 @@ extern "C" int vp_route(const vp_route_params* p, const void* logits, int dtype,
             a.lanes_per_group = lanes > 0 && (lanes & (lanes - 1)) == 0 && a.n_group * lanes <= 32 ? lanes : 0;
             a.group_shift = 0;
             while (1 << a.group_shift < a.lanes_per_group) a.group_shift++;
-            const size_t smem = a.n_group > 1 && !a.lanes_per_group ? (size_t)warps * a.E * 4 : 0;
-            e = launch_after(route_kernel<X, n>, grid, warps * 32, smem, (cudaStream_t)cuda_stream, a);
+            const size_t smem = a.n_group > 1 && !a.lanes_per_group ? (size_t)kRouteWarps * a.E * 4 : 0;
+            e = launch_after(route_kernel<X, n>, route_ctas(T), kRouteWarps * 32, smem, (cudaStream_t)cuda_stream, a);
         });
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
@@ -593,20 +591,17 @@ extern "C" int vp_route_backward(const vp_route_params* p, const void* logits, i
     if (!logits || !expert_idx || !grad_weights || !grad_logits) return VP_E_BAD_ARG;
     const int size = size_of_type(dtype);
     if ((uintptr_t)logits % size || (uintptr_t)grad_logits % size || ((uintptr_t)expert_idx | (uintptr_t)grad_weights) % 4) return VP_E_BAD_ARG;
-    const int sms = sm_count_of_device();
-    if (!sms) return VP_E_CUDA;
     RouteGradArgs a;
     a.logits = logits; a.ld = ld; a.T = T; a.E = p->experts; a.topk = p->topk;
     a.sigmoid = p->scoring == VP_SCORE_SIGMOID; a.renormalise = p->renormalise != 0; a.wide = rows_aligned(logits, ld, size, 16);
     a.scale = p->scale; a.idx = expert_idx; a.grad = grad_weights; a.out = grad_logits; a.out_ld = grad_ld;
     a.out_wide = rows_aligned(grad_logits, grad_ld, size, 16) && a.E * size % 16 == 0;
-    const int warps = route_warps(T, sms), grid = (int)(((long long)T + warps - 1) / warps);
     cudaError_t e = cudaErrorInvalidValue;
     with_type(dtype, [&](auto* type) {
         using X = std::remove_pointer_t<decltype(type)>;
         with_vpl(a.E, [&](auto vpl) {
             constexpr int n = decltype(vpl)::value;
-            e = launch_after(route_backward_kernel<X, n>, grid, warps * 32, (size_t)warps * 32 * n * 4, (cudaStream_t)cuda_stream, a);
+            e = launch_after(route_backward_kernel<X, n>, route_ctas(T), kRouteWarps * 32, (size_t)kRouteWarps * 32 * n * 4, (cudaStream_t)cuda_stream, a);
         });
     });
     return e == cudaSuccess ? VP_OK : VP_E_CUDA;
