@@ -508,7 +508,7 @@ typedef struct vp_route_params {
     int32_t scoring;        /* VP_SCORE_*                                                           */
     int32_t n_group;        /* groups of E / n_group consecutive experts, 1 .. 32, divides E         */
     int32_t topk_group;     /* groups a token may use                                               */
-    int32_t group_top;      /* a group is judged by the sum of its best 1 or 2 keys                  */
+    int32_t group_top;      /* a group is judged by its best key (1) or its best two scores + biases (2) */
     int32_t renormalise;    /* 1: weights are divided by their sum                                  */
     float   scale;          /* factor of the weights                                                */
 } vp_route_params;
@@ -517,9 +517,11 @@ typedef struct vp_route_params {
  * vp_route - experts and weights of T tokens from their router logits.
  *
  * Scores are the softmax of a token's logits or 1 / (1 + exp(-logit)); keys are scores + bias (bias: float [E] or NULL; a
- * balance bias moves the choice and not the weights).  Of the topk_group groups with the largest sums of their best
- * group_top keys the topk largest keys are chosen, in descending order; the lower index goes first among equal keys, and
- * among equal groups.  Without a bias keys are the logits.  The choice is the one that keys in 64 bits give.
+ * balance bias moves the choice and not the weights).  Without a bias keys are the logits, which order experts as their scores do.
+ * Groups are judged by their best key (group_top 1), or by the sum of their best two scores + biases (group_top 2: of scores without a
+ * bias, not of logits, whose sums order groups differently; of the one that there is, if one alone can be chosen).  Of the best topk_group groups
+ * the topk largest keys are chosen, in descending order; the lower index goes first among equal keys, and among equal groups.  The choice is
+ * the one that keys in 64 bits give.
  *   logits      [T][ld] of `dtype`, the first E of a row count.  -inf and NaN: the expert cannot be chosen (and has no part in the
  *               softmax); +inf counts as the largest finite number.  A bias that is -inf or NaN keeps its expert out as well.
  *   expert_idx  [T][topk] int32; -1 where fewer than topk experts can be chosen (vp_pack drops such copies)
@@ -569,7 +571,7 @@ int vp_combine_backward(const void* grad, const void* rows, int dtype, const int
  * 2^-127; code = value / scale to nearest, ties to even, magnitudes above 6 to 6.  A block with an infinity or a NaN gets the
  * scale 255 and codes 0.
  *   x       [rows][ld]: cols values per row (a multiple of 32); gated: 2 * cols, and the value quantised is
- *           silu(x[k]) * x[cols + k] in 32 bits (the activation between an expert's products)
+ *           silu(x[k]) * x[cols + k] in 32 bits (the activation between an expert's products; silu(-inf) is NaN)
  *   n_rows  int32[1] or NULL: rows in use (clamped to 0 .. rows); what lies behind them is neither read nor written
  *   codes   [rows][codes_ld], scales [rows][scales_ld] bytes; rows and their parts may not overlap
  * Rows, and bytes from a row to the next: below 2^31, else VP_E_UNSUPPORTED.
@@ -577,7 +579,8 @@ int vp_combine_backward(const void* grad, const void* rows, int dtype, const int
 int vp_mxfp4_quantize(const void* x, int dtype, int64_t ld, int64_t rows, int64_t cols, int gated, const int32_t* n_rows,
                       uint8_t* codes, int64_t codes_ld, uint8_t* scales, int64_t scales_ld, void* cuda_stream);
 
-/* vp_mxfp4_dequantize - the values that codes and scales stand for, rounded once to `dtype` (exact in bf16 and fp32). */
+/* vp_mxfp4_dequantize - the values that codes and scales stand for, rounded once to `dtype` (exact in bf16 and fp32 below 2^128, which scales
+ * from 253 on can pass: an infinity). */
 int vp_mxfp4_dequantize(const uint8_t* codes, int64_t codes_ld, const uint8_t* scales, int64_t scales_ld, int64_t rows,
                         int64_t cols, const int32_t* n_rows, void* out, int dtype, int64_t ld, void* cuda_stream);
 
@@ -587,14 +590,15 @@ int vp_mxfp4_dequantize(const uint8_t* codes, int64_t codes_ld, const uint8_t* s
  *   x_codes    [capacity_rows][x_codes_ld] bytes, x_scales [capacity_rows][x_scales_ld]: expert-major rows (vp_unpack's order) of
  *              K values; x_codes 16-byte aligned, x_codes_ld a multiple of 16
  *   w_codes    [E][F][K / 2] (16-byte aligned), w_scales [E][F][K / 32], contiguous: the experts' matrices
- *   expert_off [E + 1] int32 (vp_unpack's): read on the device.  Rows before the first and behind the last offset are neither
- *              read nor written.
+ *   expert_off [E + 1] int32 (vp_unpack's): read on the device.  Rows before the first and behind the last offset are not
+ *              written; up to 255 rows of codes behind an expert's last one, all in the buffer, are read, and what they hold does not matter.
  *   out        [capacity_rows][out_ld] of `dtype`; may not overlap the inputs
  *   status     int32[1], bits are OR-ed in (not cleared): VP_ST_PACK_MISMATCH if an offset falls or lies outside
- *              0 .. capacity_rows (offsets are then clamped, and a row belongs to the first expert that reaches it), VP_ST_INTERNAL_TIMEOUT if a bounded wait inside the kernel gave up (out
- *              is incomplete)
+ *              0 .. capacity_rows (offsets are then clamped, and a row belongs to the first expert that reaches it),
+ *              VP_ST_INTERNAL_TIMEOUT if a bounded wait inside the kernel gave up (out is incomplete)
  * Limits: E <= 1024, K and F <= 2^20, else VP_E_UNSUPPORTED; K a multiple of 32.  capacity_rows also chooses the launch shape (from 192
- * rows per expert on pairs of CTAs): a step with few rows in a large buffer is best given the part of it that it can use.
+ * rows per expert on pairs of CTAs): a step with few rows in a large buffer is best given the part of it that it can use (16 experts of 8 rows,
+ * 7,168 x 4,096: 48 us in a buffer of 128 rows, 68 in one of 16,384).
  */
 int vp_mxfp4_product(const uint8_t* x_codes, int64_t x_codes_ld, const uint8_t* x_scales, int64_t x_scales_ld,
                      int64_t capacity_rows, const uint8_t* w_codes, const uint8_t* w_scales, int E, int64_t F, int64_t K,

@@ -29,11 +29,6 @@ __device__ __forceinline__ float warp_max(float x) {
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float warp_min(float x) {
-    float r;
-    asm volatile("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
-    return r;
-}
 template <typename T>
 __device__ __forceinline__ T warp_sum(T x) {          // the same tree for every lane: the order of the additions is fixed
 #pragma unroll

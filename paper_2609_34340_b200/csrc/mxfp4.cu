@@ -239,7 +239,9 @@ int fill(MxArgs& a, const void* x, int dtype, int64_t ld, int64_t width, int64_t
     return VP_OK;
 }
 
-// Pieces a thread: one until the GPU is full of threads, then two, so that more is on its way.
+// Pieces a thread: one until the GPU is full of threads, then two, so that more is on its way.  One | two, us, rows of 7,168 bf16: 128 to codes
+// 1.74 | 1.73, 500 2.9 | 2.4, 676 3.1 | 3.6, 3,000 10.5 | 10.3, 16,384 48.9 | 45.9; back 500 3.1 | 2.6, 676 3.4 | 3.1, 16,384 51.5 | 45.4; gated rows of
+// 2,048: 300 2.2 | 2.6, 2,000 7.0 | 7.2, 16,384 36.7 | 34.2.
 template <typename F>
 int launch_pieces(const MxArgs& a, F fn) {
     const int sms = sm_count_of_device();

@@ -13,10 +13,10 @@
 // copies of scales into tensor memory and the products, warps 4 to 7 bring finished tiles from tensor memory to the output while the next
 // tile is summed.
 //
-// What bounds it: with few rows per expert HBM, by which the matrices come (16 experts x 4,096 x 7,168, 128 rows: 48 us, 5.2 TB/s; without the loads of
-// scales 43, so a seventh is their latency); with many the operands' way from L2 to the SMs, 11 TB/s here (16,384 rows, 8 experts, 7,168 x 4,096: 175 us,
-// 5.5 PFLOP/s; the loads alone 176, the products alone 122); a single row is a chain of a third of a microsecond per 256 values of k
-// (7,168 x 4,096: 12 us).  Tried: scales through asynchronous copies to shared memory, or two to four chunks ahead in registers (1.1 to 1.5 times the
+// What bounds it: with few rows per expert HBM, by which the matrices come (16 experts x 4,096 x 7,168, 128 rows: 48 us back to back, 5.2 TB/s, 53 with
+// other inputs from call to call; without the loads of scales 43, so a seventh is their latency); with many the operands' way from L2 to the SMs, 11 TB/s here (16,384 rows, 8 experts, 7,168 x 4,096: 175 us,
+// 5.5 PFLOP/s, 181 under the power cap; the loads alone 176, the products alone 122); a single row is a chain of a third of a microsecond per
+// 256 values of k (7,168 x 4,096: 11 us).  Tried: scales through asynchronous copies to shared memory, or two to four chunks ahead in registers (1.1 to 1.5 times the
 // time), scales in tensor memory a stage ahead with barriers of their own (1.4 times), one CTA on 128 x 256 (274 us).
 #include <cuda.h>
 #include <type_traits>
@@ -690,9 +690,11 @@ extern "C" int vp_mxfp4_product_polls(const uint8_t* x_codes, int64_t x_codes_ld
                         (uintptr_t)out % 16 == 0 && out_ld * size % 16 == 0, status, polls};
     // Row tiles there can be at most: a part of one per expert more than the rows fill.
     const auto most_tiles = [&](int mt, int nt) { return ((capacity_rows + mt - 1) / mt + (E < capacity_rows ? E : capacity_rows)) * ((F + nt - 1) / nt); };
-    // A pair where experts have rows for 256 (16 x 128 rows, half of a pair's rows empty: 65 us against 57 of one CTA; 8 x 384 63 against 80) and
-    // there are tiles for more than a quarter of the GPU (2,048 rows of one expert, 1,024 features of 7,168: 19 against 17 us; 4,096
-    // features: 35 against 54).
+    // A pair where experts may have rows for 256 and there are tiles for more than a quarter of the GPU.  Pairs | one CTA each, us, 4,096 features of
+    // 7,168: 16 x 128 rows 62 | 52 (half of a pair's rows empty), 8 x 128 40 | 33, 8 x 192 41 | 52, 16 x 200 64 | 77, 8 x 386 57 | 75; one expert's 512 rows
+    // 21.6 | 17.2, 1,024 19.7 | 24.3, 2,048 34.7 | 46.8, and 2,048 on 1,024 features 19.6 | 16.5, on 2,048 21.9 | 26.6.  The rows themselves are known on the
+    // device only: 16 x 8 rows take 48 us in a buffer for 128, where this choice is right, 58 in one for 3,200 (49 with one CTA each) and
+    // 68 in one for 16,384 (56).
     const bool pairs = capacity_rows >= (int64_t)192 * E && capacity_rows / 256 * ((F + 255) / 256) * 15 >= 4 * sms;
     const long long tiles = pairs ? 2 * most_tiles(256, 256) : most_tiles(128, 128);
     const int grid = (int)(tiles < sms ? tiles : sms) / (pairs ? 2 : 1) * (pairs ? 2 : 1);
