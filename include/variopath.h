@@ -523,7 +523,8 @@ typedef struct vp_route_params {
  * the topk largest keys are chosen, in descending order; the lower index goes first among equal keys, and among equal groups.  The choice is
  * the one that keys in 64 bits give.
  *   logits      [T][ld] of `dtype`, the first E of a row count.  -inf and NaN: the expert cannot be chosen (and has no part in the
- *               softmax); +inf counts as the largest finite number.  A bias that is -inf or NaN keeps its expert out as well.
+ *               softmax); +inf counts as the largest finite number.  A bias that is -inf or NaN keeps its expert out as well; +inf
+ *               counts as the largest finite number there, too.
  *   expert_idx  [T][topk] int32; -1 where fewer than topk experts can be chosen (vp_pack drops such copies)
  *   weights     [T][topk] float; 0 there
  */

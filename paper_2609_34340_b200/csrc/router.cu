@@ -268,11 +268,14 @@ route_kernel(const __grid_constant__ RouteArgs a) {
             if (rounded_keys) key[v] = by[v];
         }
         largest = warp_max(largest);
-        if (!(largest < CUDART_INF_F)) {          // a bias of -inf (or inf: then all keys are compared in 64 bits), or no logit
+        if (!(largest < CUDART_INF_F)) {          // a bias of -inf, or of inf, which counts as the largest number, or no logit
             largest = 0;
 #pragma unroll
-            for (int v = 0; v < VPL; v++)
+            for (int v = 0; v < VPL; v++) {
+                by[v] = fminf(by[v], CUDART_MAX_NORMAL_F);
+                if (rounded_keys) key[v] = by[v];
                 if (by[v] > -CUDART_INF_F) largest = fmaxf(largest, fabsf(by[v]));
+            }
             largest = warp_max(largest);
         }
         tol = over * twice_score_error(a.sigmoid, VPL) + 2.5e-7f * largest;       // (the sum with the bias: half a unit of the key)

@@ -131,6 +131,25 @@ def test_route_of_biases_of_the_lowest_value(vp, scoring, experts, n_group, topk
 
 
 @pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("n_group,topk_group,group_top", [(1, 1, 1), (8, 4, 2), (4, 2, 1)])
+def test_route_of_infinite_biases(vp, scoring, n_group, topk_group, group_top):
+    """An infinite bias is the largest number: its expert goes before finite ones, and in the order of indices beside that number itself."""
+    g = _gen(21)
+    top = torch.finfo(torch.float32).max
+    for E in (8, 40, 96, 256):
+        p = vp.RouteParams(E, min(E * topk_group // n_group, 9), scoring, n_group, topk_group, group_top, True, 1.0)
+        for scale in (0.0, 1.0):
+            z = torch.randn(12, E, generator=g) * scale
+            bias = torch.randn(E, generator=g) * 0.02
+            for share in (0.05, 0.5, 1.0):
+                b = bias.clone()
+                pick = torch.rand(E, generator=g)
+                b[pick < share] = math.inf
+                b[pick < share / 2] = top
+                _check(vp, p, z, b)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("n_group,topk_group,group_top", [(1, 1, 1), (8, 4, 2)])
 def test_route_of_equal_logits_takes_the_lowest_index(vp, scoring, n_group, topk_group, group_top):
     p = vp.RouteParams(256, 8, scoring, n_group, topk_group, group_top, True, 1.0)
